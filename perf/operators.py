@@ -4,7 +4,7 @@ layer when many sequences share one pool of cache pages.
 A case is a dict of plain values; `op` says which operator a pass calls:
 
   norm    hi_add_rmsnorm   residual + x, its root-mean-square norm, the new residual
-  w4      hi_linear_w4     rows times a weight matrix of 4-bit codes with a scale and a zero for each 128 of a row
+  w4      hi_linear_quantized  rows times a weight matrix of 4-bit codes with a scale and a zero for each 128 of a row
   append  hi_paged_append  rotary embedding of new rows at their sequences' positions; K and V enter the pages, in bf16
                            or as 8-bit rows (e4m3) with a scale each
   attn    hi_paged_attn    causal grouped-query attention of each sequence's new rows over its pages
@@ -224,7 +224,7 @@ def _run_own(s):
                           c["d"], EPS, s["new_residual"], s["out"])
         return s["out"], s["new_residual"]
     if c["op"] == "w4":
-        hb.hi_linear_w4(stream, s["x"], s["codes"], s["scale"], s["zero"], c["rows"], c["n_in"], c["n_out"],
+        hb.hi_linear_quantized(stream, s["x"], s["codes"], s["scale"], s["zero"], c["rows"], c["n_in"], c["n_out"],
                         int(c["x_heads"]), int(c["y_heads"]), s["out"])
         return s["out"]
     cache, batch = _handles(s)

@@ -378,6 +378,107 @@ hi_status hi_qkv_rope_static(void* stream, const void* x_dev, const void* w_qkv_
 hi_status hi_kv_quantize(void* stream, const void* rows_dev, int64_t n_rows, void* packed_dev);
 hi_status hi_kv_dequantize(void* stream, const void* packed_dev, int64_t n_rows, void* rows_dev);
 
+/*
+ * Serving a batch of sequences from one pool of cache pages (Section 3.2 notes that the head-wise partition extends to the
+ * batch dimension; the contexts above serve one sequence each).  All of it stateless: device buffers and a stream.  A layer's
+ * step over the new rows of all sequences, back to back in [rows]-first buffers, is
+ *   hi_add_rmsnorm -> hi_qkv_rope (rope_theta = 0) or hi_linear_quantized -> hi_paged_append -> hi_paged_attn
+ *   -> hi_out_proj or hi_linear_quantized -> the next hi_add_rmsnorm.
+ *
+ * hi_add_rmsnorm: h = x + residual (in fp32), residual_out = h rounded, out = bf16(h / sqrt(mean(h^2) + eps) * weight), row
+ *   by row; mean, root and products in fp32 from the unrounded h, so that each output is rounded once.
+ *   x_dev [n_rows][d], bf16 or fp32 (x_fp32); residual_dev the same shape, bf16 or fp32 (residual_fp32), or null: h = x;
+ *   weight_dev bf16 [d]; residual_out_dev in the residual's type, or null: not written; out_dev bf16 [n_rows][d].
+ *   residual_out_dev may be residual_dev (in place) and out_dev may be a bf16 x_dev; other overlaps are not allowed.  d a
+ *   multiple of 8, at most 16384 (HI_ERR_UNSUPPORTED); eps >= 0; n_rows = 0 does nothing.
+ */
+hi_status hi_add_rmsnorm(void* stream, const void* x_dev, int32_t x_fp32, const void* residual_dev, int32_t residual_fp32,
+                         const void* weight_dev, int32_t n_rows, int32_t d, float eps, void* residual_out_dev, void* out_dev);
+
+/*
+ * Weights in 4 bits with group scales: a matrix W [n_out][n_in] (bf16, the layout of the projections above) is held as
+ *   codes [n_out][n_in / 2] bytes, input channel 2i in the low nibble of byte i, channel 2i + 1 in the high one,
+ *   scales and zeros bf16 [n_out][n_in / 128], one pair for each 128 consecutive input channels of a row,
+ * and stands for W^ = zero + code * scale (code 0 .. 15), the encoding of the 4-bit rows on the link with groups of 128.
+ * hi_weight_quantize makes it from bf16 weights, per group in binary32 with one rounding per operation: zero = min, scale =
+ * bf16((max - min) * (1/15)) (0 below 2^-120), code = min(15, rint((w - zero) * (1 / scale))); weights must be finite with a
+ * range below 2^127 a group.
+ * hi_linear_quantized: Y = X W^^T with fp32 sums and one rounding to bf16; W^ itself is never rounded (the products are formed
+ * with the codes, which bf16 holds exactly; scales and zeros enter in fp32 once a group).
+ *   x_dev bf16 [n_rows][n_in], or with x_heads = 1 head-major [n_in / 128][n_rows][128] (what the attention calls write);
+ *   y_dev bf16 [n_rows][n_out], or with y_heads = 1 head-major [n_out / 128][n_rows][128] (what hi_paged_append and the
+ *   attention calls read: with the rows of W_Q, W_K, W_V in W, q, k and v follow each other).
+ * n_in a multiple of 128; n_out a multiple of 16, of 128 with y_heads (HI_ERR_UNSUPPORTED); any number of rows, n_rows = 0 does
+ * nothing.  codes, x and y 16-byte aligned, scales and zeros 2-byte.
+ */
+hi_status hi_weight_quantize(void* stream, const void* w_dev, int32_t n_out, int32_t n_in, void* codes_dev, void* scales_dev,
+                             void* zeros_dev);
+hi_status hi_linear_quantized(void* stream, const void* x_dev, const void* codes_dev, const void* scales_dev,
+                              const void* zeros_dev, int32_t n_rows, int32_t n_in, int32_t n_out, int32_t x_heads,
+                              int32_t y_heads, void* y_dev);
+
+/*
+ * A pool of cache pages in HBM, shared by sequences.  Row r of page p for KV head h lies at
+ *   pages [p][h][K|V][r][128], bf16 (kv_bits = 16) or e4m3 (kv_bits = 8), and with kv_bits = 8 its scale at
+ *   scales [p][h][K|V][r], fp32: a stored value stands for e4m3 * scale.
+ * page_rows is a power of two from 16 to 1024.  Both buffers 16-byte aligned.
+ */
+typedef struct hi_paged_cache {
+  void* pages;           /* DEVICE */
+  void* scales;          /* DEVICE; null with kv_bits = 16 */
+  int32_t n_pages;
+  int32_t n_kv_heads;
+  int32_t page_rows;
+  int32_t kv_bits;       /* 16 or 8 */
+} hi_paged_cache;
+
+/*
+ * The sequences of a step.  Sequence s has past_lens[s] rows in the cache and brings the rows row_starts[s] .. row_starts[s + 1]
+ * - 1 of the step's buffers, at positions past_lens[s] and on; its position i lies in page page_table[s][i / page_rows] at row
+ * i % page_rows.  All three arrays are read on the stream when the kernels run, so a captured step can be replayed with other
+ * lengths.  Nothing out of range is ever followed: row_starts are taken within 0 .. n_rows and as 0 rows where they descend; a
+ * sequence with past_lens[s] < 0 is left out; positions beyond the table and pages that are not 0 .. n_pages - 1 hold nothing
+ * (rows there are neither written nor attended over, and a query row that sees no key at all has an output of zeros).  Rows of
+ * the buffers that belong to no sequence are left as they were.  Pages may be shared by sequences to be read; two sequences
+ * that append to the same row of a page race for it.
+ */
+typedef struct hi_paged_batch {
+  const int32_t* page_table;  /* DEVICE [n_seqs][table_pages] */
+  const int32_t* past_lens;   /* DEVICE [n_seqs] */
+  const int32_t* row_starts;  /* DEVICE [n_seqs + 1], ascending */
+  int32_t n_seqs;
+  int32_t table_pages;
+  int32_t n_rows;             /* rows of the step's buffers, the padding behind the last sequence included */
+  int32_t max_rows;           /* the most new rows of one sequence, as a hint that picks the kernel (>= 1): a batch with
+                                 longer ones has the same results, later */
+} hi_paged_batch;
+
+/*
+ * hi_paged_append: takes the step's projected rows into the cache.  q_in_dev [n_q_heads][n_rows][128], k_in_dev and v_in_dev
+ *   [n_kv_heads][n_rows][128], bf16 or fp32 (in_fp32: hi_qkv_rope's out_fp32, so that a row is rounded once).  Queries and
+ *   keys are rotated to their positions as by hi_qkv_rope (rope_theta = 0: not); queries are multiplied by q_scale (> 0;
+ *   HI_Q_PRESCALE for hi_paged_attn with q_prescaled = 1), rounded to bf16 and written to q_out_dev [n_q_heads][n_rows][128],
+ *   which may be a bf16 q_in_dev (in place); q_in_dev and q_out_dev may both be null.  K and V rows enter the pages, with
+ *   kv_bits = 8 as scale = max |x| / 448 and e4m3(x / scale), rounded to nearest even (a row whose largest magnitude is below
+ *   2^-100 is stored as zeros with scale 0).
+ * hi_paged_attn: out[j][t][:] = softmax_i(q[j][t] . K[i] / sqrt(128)) V[i] over the cached rows i = 0 .. position of t of t's
+ *   sequence, for query head j and KV head j / (n_q_heads / n_kv_heads); call hi_paged_append first, the step's own rows are
+ *   read from the pages too.  q_dev and out_dev bf16 [n_q_heads][n_rows][128]; q_prescaled as in hi_problem.  Scores, maxima,
+ *   sums and outputs are held in fp32; weights are rounded to bf16 for the second product.  1 to 16 query heads a KV head.
+ *   workspace_dev: DEVICE, hi_paged_workspace_bytes bytes, filled with zeros once before its first use; a call leaves it fit
+ *   for the next one.  Calls that may overlap in time need workspaces of their own, as do captured graphs that may.
+ *   A row's sums may be cut differently when batch or hint change; the same call gives the same bits.
+ * All buffers 16-byte aligned, the arrays of the batch 4-byte; cache and batch are HOST structs, read before the call returns;
+ * n_seqs = 0 or n_rows = 0 does nothing.  Errors: HI_ERR_ARG, HI_ERR_UNSUPPORTED, HI_ERR_RANGE (a batch whose size, times
+ * the length of the table, cannot be counted in 31 bits of 16-row blocks), HI_ERR_HIP.
+ */
+hi_status hi_paged_append(void* stream, const hi_paged_cache* cache, const hi_paged_batch* batch, const void* q_in_dev,
+                          const void* k_in_dev, const void* v_in_dev, int32_t in_fp32, int32_t n_q_heads, double rope_theta,
+                          float q_scale, void* q_out_dev);
+hi_status hi_paged_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int64_t* bytes);
+hi_status hi_paged_attn(void* stream, const hi_paged_cache* cache, const hi_paged_batch* batch, const void* q_dev,
+                        int32_t n_q_heads, int32_t q_prescaled, void* out_dev, void* workspace_dev);
+
 /* T4 - drain the three streams; surfaces deferred HIP errors (HI_ERR_HIP). */
 hi_status hi_sync(hi_ctx* ctx);
 

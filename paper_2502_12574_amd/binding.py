@@ -24,7 +24,9 @@ HI_Q_PRESCALE = 0.12751743082459868      # log2(e) / sqrt(128): a pre-scaled que
 
 EXPORTS = ("hi_offload_plan", "hi_ctx_create", "hi_ctx_destroy", "hi_ctx_set_layer_cache", "hi_ctx_set_flags", "hi_ctx_set_run_ahead",
            "hi_prefill_head", "hi_decode_head", "hi_prefill_group", "hi_decode_group", "hi_decode_group_ragged", "hi_proj_workspace_bytes",
-           "hi_qkv_rope", "hi_qkv_rope_static", "hi_out_proj", "hi_kv_quantize", "hi_kv_dequantize", "hi_sync", "hi_get_stats", "hi_reset_stats", "hi_status_string", "hi_last_error")
+           "hi_qkv_rope", "hi_qkv_rope_static", "hi_out_proj", "hi_kv_quantize", "hi_kv_dequantize",
+           "hi_add_rmsnorm", "hi_weight_quantize", "hi_linear_quantized", "hi_paged_append", "hi_paged_workspace_bytes", "hi_paged_attn",
+           "hi_sync", "hi_get_stats", "hi_reset_stats", "hi_status_string", "hi_last_error")
 
 
 class hi_problem(C.Structure):
@@ -60,6 +62,16 @@ class hi_stats(C.Structure):
                 ("n_combine_kernels", C.c_int64), ("peak_staging_bytes", C.c_int64),
                 ("prefill_kernel_ms", C.c_double), ("decode_kernel_ms", C.c_double),
                 ("h2d_copy_ms", C.c_double), ("d2h_copy_ms", C.c_double), ("exposed_copy_ms", C.c_double)]
+
+
+class hi_paged_cache(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("scales", C.c_void_p), ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("page_rows", C.c_int32), ("kv_bits", C.c_int32)]
+
+
+class hi_paged_batch(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("past_lens", C.c_void_p), ("row_starts", C.c_void_p), ("n_seqs", C.c_int32),
+                ("table_pages", C.c_int32), ("n_rows", C.c_int32), ("max_rows", C.c_int32)]
 
 
 class HiError(RuntimeError):
@@ -119,6 +131,13 @@ def lib() -> C.CDLL:
         L.hi_out_proj.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp]
         L.hi_kv_quantize.argtypes = [vp, vp, i64, vp]
         L.hi_kv_dequantize.argtypes = [vp, vp, i64, vp]
+        cache, batch, f32 = C.POINTER(hi_paged_cache), C.POINTER(hi_paged_batch), C.c_float
+        L.hi_add_rmsnorm.argtypes = [vp, vp, i32, vp, i32, vp, i32, i32, f32, vp, vp]
+        L.hi_weight_quantize.argtypes = [vp, vp, i32, i32, vp, vp, vp]
+        L.hi_linear_quantized.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp]
+        L.hi_paged_append.argtypes = [vp, cache, batch, vp, vp, vp, i32, i32, C.c_double, f32, vp]
+        L.hi_paged_workspace_bytes.argtypes = [i32, i32, C.POINTER(i64)]
+        L.hi_paged_attn.argtypes = [vp, cache, batch, vp, i32, i32, vp, vp]
         L.hi_sync.argtypes = [vp]
         L.hi_get_stats.argtypes = [vp, C.POINTER(hi_stats)]
         L.hi_reset_stats.argtypes = [vp]
@@ -324,6 +343,71 @@ def hi_kv_dequantize(stream, packed_dev, n_rows, rows_dev, check: bool = True):
     st = lib().hi_kv_dequantize(_stream(stream), _ptr(packed_dev), n_rows, _ptr(rows_dev))
     if check and st != HI_OK:
         raise HiError(st, "hi_kv_dequantize")
+    return st
+
+
+def hi_add_rmsnorm(stream, x_dev, x_fp32, residual_dev, residual_fp32, weight_dev, n_rows, d, eps, residual_out_dev, out_dev,
+                   check: bool = True):
+    st = lib().hi_add_rmsnorm(_stream(stream), _ptr(x_dev), x_fp32, _ptr(residual_dev), residual_fp32, _ptr(weight_dev), n_rows,
+                              d, eps, _ptr(residual_out_dev), _ptr(out_dev))
+    if check and st != HI_OK:
+        raise HiError(st, "hi_add_rmsnorm")
+    return st
+
+
+def hi_weight_quantize(stream, w_dev, n_out, n_in, codes_dev, scales_dev, zeros_dev, check: bool = True):
+    st = lib().hi_weight_quantize(_stream(stream), _ptr(w_dev), n_out, n_in, _ptr(codes_dev), _ptr(scales_dev), _ptr(zeros_dev))
+    if check and st != HI_OK:
+        raise HiError(st, "hi_weight_quantize")
+    return st
+
+
+def hi_linear_quantized(stream, x_dev, codes_dev, scales_dev, zeros_dev, n_rows, n_in, n_out, x_heads, y_heads, y_dev,
+                        check: bool = True):
+    st = lib().hi_linear_quantized(_stream(stream), _ptr(x_dev), _ptr(codes_dev), _ptr(scales_dev), _ptr(zeros_dev), n_rows, n_in,
+                                   n_out, x_heads, y_heads, _ptr(y_dev))
+    if check and st != HI_OK:
+        raise HiError(st, "hi_linear_quantized")
+    return st
+
+
+def make_paged_cache(pages, scales, n_pages, n_kv_heads, page_rows, kv_bits=16) -> hi_paged_cache:
+    """pages: [n_pages][n_kv_heads][2][page_rows][128] bf16 (kv_bits 16) or e4m3 (8); scales: fp32 without the last axis, or None."""
+    c = hi_paged_cache(_ptr(pages), _ptr(scales), n_pages, n_kv_heads, page_rows, kv_bits)
+    c._keepalive = (pages, scales)                    # the struct only holds addresses
+    return c
+
+
+def make_paged_batch(page_table, past_lens, row_starts, n_seqs, table_pages, n_rows, max_rows) -> hi_paged_batch:
+    """page_table [n_seqs][table_pages], past_lens [n_seqs], row_starts [n_seqs + 1]: int32 on the device."""
+    b = hi_paged_batch(_ptr(page_table), _ptr(past_lens), _ptr(row_starts), n_seqs, table_pages, n_rows, max_rows)
+    b._keepalive = (page_table, past_lens, row_starts)
+    return b
+
+
+def hi_paged_append(stream, cache: hi_paged_cache, batch: hi_paged_batch, q_in_dev, k_in_dev, v_in_dev, in_fp32, n_q_heads,
+                    rope_theta, q_scale, q_out_dev, check: bool = True):
+    st = lib().hi_paged_append(_stream(stream), cache, batch, _ptr(q_in_dev), _ptr(k_in_dev), _ptr(v_in_dev), in_fp32, n_q_heads,
+                               rope_theta, q_scale, _ptr(q_out_dev))
+    if check and st != HI_OK:
+        raise HiError(st, "hi_paged_append")
+    return st
+
+
+def hi_paged_workspace_bytes(n_q_heads: int, n_kv_heads: int) -> int:
+    n = C.c_int64()
+    st = lib().hi_paged_workspace_bytes(n_q_heads, n_kv_heads, C.byref(n))
+    if st != HI_OK:
+        raise HiError(st, "hi_paged_workspace_bytes")
+    return n.value
+
+
+def hi_paged_attn(stream, cache: hi_paged_cache, batch: hi_paged_batch, q_dev, n_q_heads, q_prescaled, out_dev, workspace_dev,
+                  check: bool = True):
+    st = lib().hi_paged_attn(_stream(stream), cache, batch, _ptr(q_dev), n_q_heads, q_prescaled, _ptr(out_dev),
+                             _ptr(workspace_dev))
+    if check and st != HI_OK:
+        raise HiError(st, "hi_paged_attn")
     return st
 
 

@@ -1,0 +1,24 @@
+// What the kernels of paged attention take.
+#pragma once
+#include "hi_paged.h"
+
+namespace hi {
+
+// hi_paged_decode.hip: runs of tiles, one a workgroup (one workgroup for each of the 256 compute units, whose LDS it fills), no shorter
+// than two tiles for each of its wavefronts; pieces of blocks that lie in several runs, at most two a run
+constexpr int kPagedRuns = 256;
+constexpr int kPagedLeastRun = 8;
+constexpr int kPagedPieceFloats = 16 * kPartialFloats;
+
+struct PagedAttnArgs {
+  PagedPool pool; PagedSeqs seqs;
+  const uint16_t* q; uint16_t* out;
+  int q_heads, group;
+  int positions, by_group;       // positions of a block; 65536 / group, rounded up
+  float c;                       // what a score is multiplied by before the power of two
+  int* arrivals; float* pieces;  // in the workspace
+};
+
+hi_status launch_paged_decode(void* stream, const PagedAttnArgs& a);
+
+}  // namespace hi

@@ -1,16 +1,9 @@
 // Causal grouped-query attention of many sequences' new rows over a pool of cache pages.
-#include "hi_paged.h"
+#include "hi_paged_attn.h"
 
 namespace hi {
 
 namespace {
-
-struct PagedAttnArgs {
-  PagedPool pool; PagedSeqs seqs;
-  const uint16_t* q; uint16_t* out;
-  int q_heads, group;
-  float c;                       // what a score is multiplied by before the power of two
-};
 
 // One wavefront for each new row of each query head, a lane for two dims: one pass over the row's keys with a running maximum and sum.
 template <int BITS>
@@ -59,6 +52,8 @@ __global__ __launch_bounds__(64) void paged_attn_row_kernel(PagedAttnArgs a) {
   *(uint32_t*)(a.out + at) = pack_bf16(o0 * inv, o1 * inv);
 }
 
+constexpr int kArrivalBytes = kPagedRuns * 4;
+
 }  // namespace
 
 }  // namespace hi
@@ -68,7 +63,7 @@ using namespace hi;
 extern "C" hi_status hi_paged_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int64_t* bytes) {
   if (!bytes || n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads != 0) { set_last_error("paged workspace: bad argument"); return HI_ERR_ARG; }
   if (n_q_heads / n_kv_heads > 16) { set_last_error("paged attention: at most 16 query heads a KV head"); return HI_ERR_UNSUPPORTED; }
-  *bytes = 256;
+  *bytes = kArrivalBytes + (int64_t)2 * kPagedRuns * kPagedPieceFloats * 4;
   return HI_OK;
 }
 
@@ -90,7 +85,15 @@ extern "C" hi_status hi_paged_attn(void* stream, const hi_paged_cache* cache, co
   a.q = (const uint16_t*)q_dev; a.out = (uint16_t*)out_dev;
   a.q_heads = n_q_heads; a.group = group;
   a.c = softmax_scale_log2(q_prescaled != 0);
+  a.positions = 16 / group;
+  a.by_group = (65536 + group - 1) / group;
+  a.arrivals = (int*)workspace_dev;
+  a.pieces = (float*)((char*)workspace_dev + kArrivalBytes);
+  // tiles of 16 rows, at the table's full length, have to be countable in 31 bits
+  const int64_t blocks = (int64_t)batch->n_seqs + batch->n_rows / a.positions, tiles = ceil_div((int64_t)batch->table_pages << a.pool.shift, 16);
+  if ((double)blocks * (double)tiles * (double)cache->n_kv_heads > 2147483647.0) { set_last_error("paged attention: more tiles than can be counted"); return HI_ERR_RANGE; }
   StreamDevice on(stream);
+  if (batch->max_rows * (int64_t)group <= 16) return launch_paged_decode(stream, a);
   const dim3 grid((unsigned)batch->n_rows, (unsigned)n_q_heads);
   if (a.pool.bits == 16) hipLaunchKernelGGL(paged_attn_row_kernel<16>, grid, dim3(64), 0, (hipStream_t)stream, a);
   else hipLaunchKernelGGL(paged_attn_row_kernel<8>, grid, dim3(64), 0, (hipStream_t)stream, a);

@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libheadinfer.so")
 PYCALL = os.path.join(HERE, "_pycall" + sysconfig.get_config_var("EXT_SUFFIX"))     # native marshalling for binding.py (host code)
 SOURCES = ["hi_plan.cpp", "hi_ctx.hip", "hi_decode.hip", "hi_prefill.hip", "hi_proj.hip", "hi_kvq.hip", "hi_norm.hip", "hi_quant.hip",
-           "hi_paged.hip", "hi_paged_attn.hip", "hi_paged_decode.hip"]
+           "hi_paged.hip", "hi_paged_attn.hip", "hi_paged_decode.hip", "hi_paged_chunk.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -10,15 +10,23 @@ constexpr int kPagedRuns = 256;
 constexpr int kPagedLeastRun = 8;
 constexpr int kPagedPieceFloats = 16 * kPartialFloats;
 
+// hi_paged_chunk.hip: two workgroups of 128 rows a compute unit; blocks that are cut leave an image of their state (64 O^T accumulators,
+// m and l for each of 256 lanes) for each piece, in at most kPagedMostPieces of them
+constexpr int kPagedSlots = 512;
+constexpr int kPagedMostPieces = 1024;
+constexpr int kPagedImageFloats = 66 * 256;
+
 struct PagedAttnArgs {
   PagedPool pool; PagedSeqs seqs;
   const uint16_t* q; uint16_t* out;
   int q_heads, group;
   int positions, by_group;       // positions of a block; 65536 / group, rounded up
   float c;                       // what a score is multiplied by before the power of two
-  int* arrivals; float* pieces;  // in the workspace
+  int split;                     // pieces of a block's tiles, each a workgroup's
+  int* arrivals; float* pieces; float* images;   // in the workspace
 };
 
 hi_status launch_paged_decode(void* stream, const PagedAttnArgs& a);
+hi_status launch_paged_chunk(void* stream, const PagedAttnArgs& a, int64_t units);
 
 }  // namespace hi

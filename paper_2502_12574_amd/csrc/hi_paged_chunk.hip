@@ -1,0 +1,391 @@
+// Attention of a chunk of new rows of each of many sequences over a pool of cache pages: the matrix rate is the bound.
+//
+// Work.  A block is 128 rows of one sequence and one KV head: 128 / group consecutive positions with the query heads of that KV head,
+// so that its rows share the keys.  It sweeps its sequence's keys in tiles of 64; a workgroup takes a block, or one of `split` equal
+// pieces of its tiles where the blocks alone would not fill the chip (merged by paged_merge_kernel).  KV heads change fastest in the
+// numbering, deep blocks come first: with 8 heads each XCD sweeps one of them, and the workgroups that sweep the same tiles at the
+// same time find them in its L2.
+//
+// A wavefront holds 32 rows.  S^T = K Q^T (32x32x16 tiles) leaves a row in one lane column: its running maximum and sum are per lane,
+// and the weights, rounded to bf16, are the B operand of O^T += V^T P^T as they lie.  bf16 tiles go to LDS by direct loads; rows of
+// 8 bits pass through registers, where they become bf16 (exactly) once for the whole workgroup, and their scales multiply scores
+// and weights in fp32.  Two workgroups a compute unit hide each other's softmax.
+#include "hi_paged_attn.h"
+
+namespace hi {
+
+namespace {
+
+constexpr int kRows = 128;                       // rows of a block
+constexpr int kTileRows = 64;
+constexpr int kTileBytes = kTileRows * kRowBytes;   // 16 KiB of K (or V), bf16
+constexpr int kStageBytes = 2 * kTileBytes;
+constexpr int kScalesAt = 2 * kStageBytes;       // [stage][K|V][64] fp32
+template <int BITS> constexpr int kLds = kScalesAt + (BITS == 8 ? 2 * 2 * kTileRows * 4 : 0);
+
+typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+typedef __attribute__((address_space(3))) float lds_float;
+
+__device__ u32x4 zero_rows[16 * kRowBytes / 16];  // what the rows of a page that is not there hold
+
+// LDS chunk (16 bytes) c of tile row r lies at position c ^ swz: operand reads are free of bank conflicts
+__device__ __forceinline__ int swz_k(int row) { return row & 15; }
+__device__ __forceinline__ int swz_v(int row) { return ((row & 3) << 2) | (row & 2); }
+
+__device__ __forceinline__ float both_halves(float x, bool max) {      // with the value of lane ^ 32
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const float a = __uint_as_float(r[0]), b = __uint_as_float(r[1]);
+  return max ? fmaxf(a, b) : a + b;
+}
+
+struct State {
+  f32x16 o[4];
+  float m, l;
+};
+
+struct Lane {
+  uint32_t koff[8];  // K operand of contraction step kk (rows 32 .. 63: 8192 further on)
+  uint32_t voff[4];  // V^T operand of dims 32 db .. (8 rows on: 2048, 16 rows on: 4096)
+};
+__device__ __forceinline__ Lane lane_offsets(int lane) {
+  Lane lc;
+  const int hl = lane >> 5, col = lane & 31, s16 = lane & 15, row = 4 * hl + (s16 >> 2);
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk) lc.koff[kk] = (uint32_t)(col * kRowBytes + (((2 * kk + hl) ^ swz_k(col)) << 4));
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+    lc.voff[db] = (uint32_t)(row * kRowBytes + (((4 * db + 2 * (col >> 4) + ((s16 & 3) >> 1)) ^ swz_v(row)) << 4) + ((s16 & 1) << 3));
+  return lc;
+}
+
+// 16 e4m3 values as bf16
+__device__ __forceinline__ void widen(u32x4 b, u32x4& lo, u32x4& hi) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b[i], 1.0f, false));
+    const uint32_t y = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b[i], 1.0f, true));
+    if (i < 2) { lo[2 * i] = x; lo[2 * i + 1] = y; }
+    else { hi[2 * i - 4] = x; hi[2 * i - 3] = y; }
+  }
+}
+
+// What a workgroup does: its block, and the tiles [t0, t1) of it.
+struct ChunkWork { int seq, kv, row0, rows, tiles, t0, t1, sees, len; bool any; };
+__device__ __forceinline__ ChunkWork chunk_work(const PagedAttnArgs& a, int unit, int piece, int lane) {
+  ChunkWork w;
+  w.any = false;
+  w.kv = unit % a.pool.heads;
+  const int nth = unit / a.pool.heads;
+  int before = 0;
+  for (int s0 = 0; s0 < a.seqs.n_seqs; s0 += 64) {
+    int mine = 0;
+    if (s0 + lane < a.seqs.n_seqs) mine = (paged_seq_of(a.seqs, s0 + lane).rows + a.positions - 1) / a.positions;
+    int upto = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+      const int y = __shfl_up(upto, off);
+      if (lane >= off) upto += y;
+    }
+    const int n = __popcll(__builtin_amdgcn_ballot_w64(before + upto <= nth));
+    if (n < 64) {
+      w.seq = __builtin_amdgcn_readfirstlane(s0 + n);
+      if (w.seq >= a.seqs.n_seqs) return w;
+      if (n > 0) before += __builtin_amdgcn_readlane(upto, n - 1);
+      break;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+    w.seq = s0 + 64;
+  }
+  if (w.seq >= a.seqs.n_seqs) return w;
+  const PagedSeq q = paged_seq_of(a.seqs, w.seq);
+  const int blocks = (q.rows + a.positions - 1) / a.positions, b = blocks - 1 - (nth - before);     // the deepest first
+  if (b < 0 || b >= blocks) return w;
+  w.row0 = q.first + b * a.positions;
+  w.rows = q.rows - b * a.positions < a.positions ? q.rows - b * a.positions : a.positions;
+  const int64_t most = (int64_t)a.seqs.table_pages << a.pool.shift, all = (int64_t)q.past + q.rows;
+  w.len = (int)(all < most ? all : most);
+  const int64_t sees = (int64_t)q.past + b * a.positions, deepest = sees + w.rows;
+  w.sees = (int)(sees < w.len ? sees : w.len - 1);                     // the last key of the block's first position
+  w.tiles = (int)(((deepest < w.len ? deepest : w.len) + kTileRows - 1) / kTileRows);
+  w.t0 = (int)((int64_t)w.tiles * piece / a.split);
+  w.t1 = (int)((int64_t)w.tiles * (piece + 1) / a.split);
+  w.any = true;
+  return w;
+}
+
+// The lane's row: position row / group of the block, query head row % group of the KV head.
+struct LaneRow { int pos, g; bool live; };
+__device__ __forceinline__ LaneRow lane_row(const PagedAttnArgs& a, const ChunkWork& w, int row) {
+  LaneRow r;
+  r.pos = (row * a.by_group) >> 16;
+  r.g = row - r.pos * a.group;
+  r.live = r.pos < w.rows;
+  return r;
+}
+
+__device__ __forceinline__ void write_row(const PagedAttnArgs& a, const ChunkWork& w, const LaneRow& r, int db, int hl, const f32x16& o, float inv) {
+  uint16_t* const to = a.out + ((int64_t)(w.kv * a.group + r.g) * a.seqs.n_rows + w.row0 + r.pos) * kHeadDim;
+#pragma unroll
+  for (int rq = 0; rq < 4; ++rq)
+    *(uint2*)(to + 32 * db + 8 * rq + 4 * hl) = make_uint2(pack_bf16(o[4 * rq] * inv, o[4 * rq + 1] * inv), pack_bf16(o[4 * rq + 2] * inv, o[4 * rq + 3] * inv));
+}
+
+template <int BITS>
+__global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds_raw[kLds<BITS>];
+  lds_char* const lds = (lds_char*)lds_raw;
+  const int lane = lane_id(), wave = wave_id(), hl = lane >> 5, col = lane & 31;
+  const int unit = blockIdx.x % a.pool.heads + blockIdx.x / (a.pool.heads * a.split) * a.pool.heads;
+  const int piece = blockIdx.x / a.pool.heads % a.split;
+  const ChunkWork w = chunk_work(a, unit, piece, lane);
+  if (!w.any || w.t0 >= w.t1) return;
+  const int n = w.t1 - w.t0;
+  const int* const table = a.seqs.table + (int64_t)w.seq * a.seqs.table_pages;
+  const int in_page = (1 << a.pool.shift) - 1;
+  auto there = [&](int page) __attribute__((always_inline)) { return page >= 0 && page < a.pool.n_pages; };
+
+  // the wavefront brings rows 16 wave .. 16 wave + 15 of every tile, which lie in one page; the pages of 64 tiles are looked up at once
+  auto group_row = [&](int j) __attribute__((always_inline)) { return (w.t0 + j) * kTileRows + 16 * wave; };
+  auto pages_from = [&](int j) __attribute__((always_inline)) {
+    const int row = group_row(j + lane);
+    return j + lane < n && row < w.len ? table[row >> a.pool.shift] : -1;
+  };
+  int pages = pages_from(0);
+  auto page_of = [&](int j) __attribute__((always_inline)) {
+    if (j > 0 && (j & 63) == 0) pages = pages_from(j);
+    return __builtin_amdgcn_readlane(pages, j & 63);
+  };
+
+  u32x4 kreg[2], vreg[2];                        // 8-bit rows on their way
+  float screg = 0.f;
+  const uint32_t lds_wave = (uint32_t)(uintptr_t)lds + wave * 4096;
+  auto fetch = [&](int j, int stage) __attribute__((always_inline)) {
+    const int page = page_of(j), row = group_row(j), last = w.len - 1 - row;     // rows past the end re-read the last one
+    const bool ok = there(page);
+    const int64_t at = paged_row(a.pool, ok ? page : 0, w.kv, row & in_page);
+    if constexpr (BITS == 16) {
+      const char* const k = ok ? a.pool.pages + at * kRowBytes : (const char*)zero_rows;
+      const char* const v = ok ? k + ((int64_t)kRowBytes << a.pool.shift) : (const char*)zero_rows;
+      const uint32_t to = lds_wave + stage * kStageBytes;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = 4 * i + (lane >> 4), p = lane & 15, from = r < last || last < 0 ? r : last;
+        g2lds16_s<0>(k, (uint32_t)(from * kRowBytes + ((p ^ swz_k(r)) << 4)), to + i * 1024);
+        g2lds16_s<0>(v, (uint32_t)(from * kRowBytes + ((p ^ swz_v(r)) << 4)), to + kTileBytes + i * 1024);
+      }
+    } else {
+      const char* const k = a.pool.pages + at * kHeadDim;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = 8 * i + (lane >> 3), from = r < last ? r : last;
+        kreg[i] = vreg[i] = (u32x4){0, 0, 0, 0};
+        if (ok) {
+          kreg[i] = *(const u32x4*)(k + from * kHeadDim + 16 * (lane & 7));
+          vreg[i] = *(const u32x4*)(k + (((int64_t)kHeadDim) << a.pool.shift) + from * kHeadDim + 16 * (lane & 7));
+        }
+      }
+      const int r = lane & 15;
+      screg = ok && lane < 32 ? a.pool.scales[at + (r < last ? r : last) + (lane < 16 ? 0 : in_page + 1)] : 0.f;
+    }
+  };
+  auto settle = [&](int stage) __attribute__((always_inline)) {        // 8-bit rows into LDS, as bf16
+    if constexpr (BITS == 8) {
+      lds_char* const to = lds + stage * kStageBytes + wave * 4096;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = 8 * i + (lane >> 3), p = lane & 7;
+        u32x4 lo, hi;
+        widen(kreg[i], lo, hi);
+        *(lds_u32x4*)(to + r * kRowBytes + (((2 * p) ^ swz_k(r)) << 4)) = lo;
+        *(lds_u32x4*)(to + r * kRowBytes + (((2 * p + 1) ^ swz_k(r)) << 4)) = hi;
+        widen(vreg[i], lo, hi);
+        *(lds_u32x4*)(to + kTileBytes + r * kRowBytes + (((2 * p) ^ swz_v(r)) << 4)) = lo;
+        *(lds_u32x4*)(to + kTileBytes + r * kRowBytes + (((2 * p + 1) ^ swz_v(r)) << 4)) = hi;
+      }
+      if (lane < 32) *(lds_float*)(lds + kScalesAt + ((stage * 2 + (lane >> 4)) * kTileRows + 16 * wave + (lane & 15)) * 4) = screg;
+    }
+  };
+  fetch(0, 0);
+
+  // rows that a piece's tiles lack because their page is not there: looked for once
+  bool holes = false;
+  for (int p = w.t0 * kTileRows >> a.pool.shift; p <= ((w.t1 * kTileRows < w.len ? w.t1 * kTileRows : w.len) - 1) >> a.pool.shift; p += 64) {
+    const int i = p + lane, end = ((w.t1 * kTileRows < w.len ? w.t1 * kTileRows : w.len) - 1) >> a.pool.shift;
+    holes |= __builtin_amdgcn_ballot_w64(i <= end && !there(table[i <= end ? i : end])) != 0;
+  }
+
+  const LaneRow mine = lane_row(a, w, 32 * wave + col);
+  bf16x8 qf[8];
+  {
+    const uint16_t* const q = a.q + ((int64_t)(w.kv * a.group + mine.g) * a.seqs.n_rows + w.row0 + mine.pos) * kHeadDim + 8 * hl;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      uint4 raw = make_uint4(0, 0, 0, 0);
+      if (mine.live) raw = *(const uint4*)(q + 16 * kk);
+      qf[kk] = __builtin_bit_cast(bf16x8, raw);
+    }
+  }
+  const int lim = w.sees + mine.pos < w.len ? w.sees + mine.pos : w.len - 1;     // the last key the lane's row sees
+  const Lane lc = lane_offsets(lane);
+  State st;
+  st.m = kNegBig;
+  st.l = 0.f;
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st.o[db][r] = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(qf[kk]));
+  settle(0);
+
+  for (int j = 0; j < n; ++j) {
+    const int stage = j & 1, key0 = (w.t0 + j) * kTileRows;
+    if constexpr (BITS == 16) wait_vmcnt<0>();
+    __syncthreads();
+    if (j + 1 < n) fetch(j + 1, 1 - stage);
+    lds_char* const kt = lds + stage * kStageBytes;
+    lds_char* const vt = kt + kTileBytes;
+
+    // register r of sub-block sb: the lane's row against key 32 sb + 8 (r / 4) + 4 hl + r % 4 of the tile
+    f32x16 s[2];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) { s[0][r] = 0.f; s[1][r] = 0.f; }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(lds_bf16x8*)(kt + lc.koff[i >> 1] + (i & 1) * 8192), qf[i >> 1], s[i & 1], 0, 0, 0);
+    lds_char* const sc = lds + kScalesAt + stage * 2 * kTileRows * 4 + 16 * hl;
+    if constexpr (BITS == 8) {
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const f32x4 f = *(lds_f32x4*)(sc + (32 * sb + 8 * q4) * 4);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[sb][4 * q4 + r] *= f[r];
+        }
+    }
+    const bool hides = key0 + kTileRows - 1 > w.sees;
+    if (hides || holes) {
+      uint64_t shown = lim - key0 >= 63 ? ~0ull : lim < key0 ? 0ull : (2ull << (lim - key0)) - 1;
+      if (holes) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = key0 + 16 * i;
+          if (row < w.len && !there(table[row >> a.pool.shift])) shown &= ~(0xFFFFull << (16 * i));
+        }
+      }
+      shown >>= 4 * hl;
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const uint32_t t = (uint32_t)__builtin_amdgcn_sbfe((int)(uint32_t)(shown >> (32 * sb)), 8 * (r >> 2) + (r & 3), 1);
+          s[sb][r] = __uint_as_float((__float_as_uint(s[sb][r]) & t) | (__float_as_uint(kNegBig) & ~t));
+        }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[sb][r]);
+    const float m_new = fmaxf(st.m, both_halves(mx, true));
+    if (__builtin_amdgcn_ballot_w64(m_new > st.m) != 0) {
+      const float alpha = fast_exp2((st.m - m_new) * a.c);
+      st.l *= alpha;
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st.o[db][r] *= alpha;
+      st.m = m_new;
+    }
+    const float mc = st.m > kNegBig ? st.m * a.c : 0.f;           // a row that has seen nothing yet adds weights of zero
+    // weights, rounded to bf16 for the matrix pipe; their sum is that of the fp32 values
+    u32x4 pw[2][2];
+    float lq[4];
+#pragma unroll
+    for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = fast_exp2(__builtin_fmaf(s[sb][8 * u + e], a.c, -mc));
+        lq[2 * sb + u] = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+        if constexpr (BITS == 8) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const f32x4 f = *(lds_f32x4*)(sc + (kTileRows + 32 * sb + 16 * u + 8 * h) * 4);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) p[4 * h + r] *= f[r];
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) pw[sb][u][e] = pack_bf16(p[2 * e], p[2 * e + 1]);
+      }
+    st.l += (lq[0] + lq[1]) + (lq[2] + lq[3]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      lds_char* const p = vt + lc.voff[i & 3] + (i >> 2) * 4096;
+      const bf16x4 v0 = lds_read_tr8(p), v1 = lds_read_tr8(p + 2048);
+      st.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16((bf16x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7),
+                                                          __builtin_bit_cast(bf16x8, pw[i >> 3][(i >> 2) & 1]), st.o[i & 3], 0, 0, 0);
+    }
+    if (j + 1 < n) settle(1 - stage);
+  }
+
+  const float l = both_halves(st.l, false);
+  if (a.split == 1) {
+    const float inv = l > 0.f ? 1.0f / l : 0.f;
+    if (mine.live) {
+#pragma unroll
+      for (int db = 0; db < 4; ++db) write_row(a, w, mine, db, hl, st.o[db], inv);
+    }
+    return;
+  }
+  float* const image = a.images + (int64_t)(unit * a.split + piece) * kPagedImageFloats + threadIdx.x;
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) image[(db * 16 + r) * 256] = st.o[db][r];
+  image[64 * 256] = st.m;
+  image[65 * 256] = l;
+}
+
+// Joins the pieces of a block: a workgroup for each 32 dims of it, in the lanes of the kernel above.
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
+  const int lane = lane_id(), wave = wave_id(), unit = blockIdx.x, db = blockIdx.y;
+  const ChunkWork w = chunk_work(a, unit, 0, lane);
+  if (!w.any) return;
+  const LaneRow mine = lane_row(a, w, 32 * wave + (lane & 31));
+  const float* const images = a.images + (int64_t)unit * a.split * kPagedImageFloats + threadIdx.x;
+  float m = kNegBig, l = 0.f;
+  for (int p = 0; p < a.split; ++p)
+    if ((int64_t)w.tiles * p / a.split < (int64_t)w.tiles * (p + 1) / a.split) m = fmaxf(m, images[(int64_t)p * kPagedImageFloats + 64 * 256]);
+  f32x16 o;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) o[r] = 0.f;
+  for (int p = 0; p < a.split; ++p) {
+    if ((int64_t)w.tiles * p / a.split >= (int64_t)w.tiles * (p + 1) / a.split) continue;
+    const float* const x = images + (int64_t)p * kPagedImageFloats;
+    const float f = fast_exp2((x[64 * 256] - m) * a.c);
+    l += f * x[65 * 256];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[r] += f * x[(db * 16 + r) * 256];
+  }
+  if (mine.live) write_row(a, w, mine, db, lane >> 5, o, l > 0.f ? 1.0f / l : 0.f);
+}
+
+}  // namespace
+
+hi_status launch_paged_chunk(void* stream, const PagedAttnArgs& a, int64_t units) {
+  const dim3 grid((unsigned)(units * a.split));
+  if (a.pool.bits == 16) hipLaunchKernelGGL(paged_chunk_kernel<16>, grid, dim3(256), 0, (hipStream_t)stream, a);
+  else hipLaunchKernelGGL(paged_chunk_kernel<8>, grid, dim3(256), 0, (hipStream_t)stream, a);
+  const hi_status st = launched("paged attention");
+  if (st != HI_OK || a.split == 1) return st;
+  hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned)units, 4), dim3(256), 0, (hipStream_t)stream, a);
+  return launched("paged attention merge");
+}
+
+}  // namespace hi

@@ -70,23 +70,270 @@ struct LinearArgs {
   int rows, n_in, n_out, x_heads, y_heads;
 };
 
-// One wavefront for an output of a row, two channels a lane at a time.
-__global__ __launch_bounds__(64) void linear_simple_kernel(LinearArgs a) {
-  const int n = blockIdx.x, lane = threadIdx.x, groups = a.n_in / kQGroup;
-  for (int r = blockIdx.y; r < a.rows; r += gridDim.y) {
-    float sum = 0.f;
-    for (int g = 0; g < groups; ++g) {
-      const int64_t at = a.x_heads ? ((int64_t)g * a.rows + r) * kQGroup : (int64_t)r * a.n_in + g * kQGroup;
-      const uint32_t xw = *(const uint32_t*)(a.x + at + 2 * lane);
-      const uint32_t c = (uint8_t)a.codes[((int64_t)n * groups + g) * (kQGroup / 2) + lane];
-      const float x0 = __uint_as_float(xw << 16), x1 = __uint_as_float(xw & 0xFFFF0000u);
-      const float s = bf16_bits_to_float(a.scales[(int64_t)n * groups + g]), z = bf16_bits_to_float(a.zeros[(int64_t)n * groups + g]);
-      sum += s * (x0 * (float)(c & 15) + x1 * (float)(c >> 4)) + z * (x0 + x1);
-    }
-    sum = over_wave(sum, op_add);
-    const int64_t to = a.y_heads ? ((int64_t)(n >> 7) * a.rows + r) * kHeadDim + (n & 127) : (int64_t)r * a.n_out + n;
-    if (lane == 0) a.y[to] = (uint16_t)pack_bf16(sum, 0.f);
+// A code c becomes the bf16 number 16 + c with two operations for two codes: 16 .. 31 is an exponent and the code in the upper bits of
+// the fraction.  So with s and z a group's scale and zero, and exactly in all but the fp32 sums,
+//   sum_k W^_k x_k = s sum_k (16 + c_k) x_k + (z - 16 s) sum_k x_k   over the group's 128 channels:
+// no weight is rounded, and scale and zero enter once a group instead of once a weight.
+// A word holds the codes of 8 channels; the pairs come out as (0, 4), (1, 5), (2, 6), (3, 7), an order that x is brought into.
+__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t w) {
+  u32x4 b;
+  b[0] = ((w << 3) & 0x00780078u) | 0x41804180u;
+  b[1] = ((w >> 1) & 0x00780078u) | 0x41804180u;
+  b[2] = ((w >> 5) & 0x00780078u) | 0x41804180u;
+  b[3] = ((w >> 9) & 0x00780078u) | 0x41804180u;
+  return __builtin_bit_cast(bf16x8, b);
+}
+__device__ __forceinline__ u32x4 in_code_order(u32x4 x) {
+  u32x4 y;
+  y[0] = __builtin_amdgcn_perm(x[2], x[0], 0x05040100);
+  y[1] = __builtin_amdgcn_perm(x[2], x[0], 0x07060302);
+  y[2] = __builtin_amdgcn_perm(x[3], x[1], 0x05040100);
+  y[3] = __builtin_amdgcn_perm(x[3], x[1], 0x07060302);
+  return y;
+}
+__device__ __forceinline__ bf16x8 bf16_ones() { return __builtin_bit_cast(bf16x8, (u32x4){0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}); }
+
+// the row's 128 channels of group g
+__device__ __forceinline__ const uint16_t* x_group(const LinearArgs& a, int row, int g) {
+  return a.x + (a.x_heads ? ((int64_t)g * a.rows + row) * kQGroup : (int64_t)row * a.n_in + (int64_t)g * kQGroup);
+}
+__device__ __forceinline__ uint16_t* y_at(const LinearArgs& a, int row, int n) {
+  return a.y + (a.y_heads ? ((int64_t)(n >> 7) * a.rows + row) * kHeadDim + (n & 127) : (int64_t)row * a.n_out + n);
+}
+
+// ---- up to 64 rows: the read of the weights is the bound.  A workgroup takes 16 NT outputs and all rows (RT tiles of 16); its 8
+// wavefronts take the groups in turn and add their sums through LDS.  A lane reads 32 consecutive codes of its output, and the same
+// 32 channels of its row of x; U groups are under way at a time.  Sums of x come out of the matrix pipe too, against ones.
+template <int RT, int NT, int U>
+__global__ __launch_bounds__(512, RT == 1 ? 4 : 2) void linear_few_kernel(LinearArgs a) {
+  __shared__ float part[8][RT * NT][256];
+  const int lane = lane_id(), wave = wave_id(), c16 = lane & 15, g4 = lane >> 4;
+  const int n0 = blockIdx.x * 16 * NT, row0 = blockIdx.y * 16 * RT, groups = a.n_in / kQGroup;
+  const char* codes[NT];
+  const uint16_t *sp[NT], *zp[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int n = n0 + 16 * t + c16 < a.n_out ? n0 + 16 * t + c16 : a.n_out - 1;
+    codes[t] = a.codes + (int64_t)n * (a.n_in / 2) + 16 * g4;
+    sp[t] = a.scales + (int64_t)n * groups;
+    zp[t] = a.zeros + (int64_t)n * groups;
   }
+  int row[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) row[t] = row0 + 16 * t + c16 < a.rows ? row0 + 16 * t + c16 : a.rows - 1;
+  f32x4 y[RT][NT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) y[i][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  struct Group {
+    u32x4 w[NT], x[RT][4];
+    uint16_t s[NT], z[NT];
+  };
+  auto load = [&](Group& b, int g) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      b.w[t] = __builtin_nontemporal_load((const u32x4*)(codes[t] + (int64_t)g * (kQGroup / 2)));
+      b.s[t] = sp[t][g];
+      b.z[t] = zp[t][g];
+    }
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      const uint16_t* const x = x_group(a, row[i], g) + 32 * g4;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) b.x[i][k] = *(const u32x4*)(x + 8 * k);
+    }
+  };
+  auto add = [&](const Group& b) __attribute__((always_inline)) {
+    f32x4 acc[RT][NT], xs[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      xs[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[i][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      bf16x8 w[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) w[t] = codes_to_bf16(b.w[t][k]);
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        const bf16x8 x = __builtin_bit_cast(bf16x8, in_code_order(b.x[i][k]));
+        xs[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, bf16_ones(), xs[i], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w[t], acc[i][t], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const float s = bf16_bits_to_float(b.s[t]), z = __builtin_fmaf(-16.0f, s, bf16_bits_to_float(b.z[t]));
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[i][t][r] = __builtin_fmaf(s, acc[i][t][r], __builtin_fmaf(z, xs[i][r], y[i][t][r]));
+    }
+  };
+  Group b[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (wave + 8 * u < groups) load(b[u], wave + 8 * u);
+  for (int g = wave; g < groups; g += 8 * U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = g + 8 * u;
+      if (at < groups) {
+        add(b[u]);
+        if (at + 8 * U < groups) load(b[u], at + 8 * U);
+      }
+    }
+  }
+  // register r: row 4 g4 + r of the tile, output c16
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) part[wave][i * NT + t][(4 * g4 + r) * 16 + c16] = y[i][t][r];
+  __syncthreads();
+  for (int i = threadIdx.x; i < RT * NT * 128; i += 512) {          // two outputs of a row each
+    const int n = 2 * (i % (8 * NT)), r = i / (8 * NT), tile = (r >> 4) * NT + (n >> 4), at = (r & 15) * 16 + (n & 15);
+    if (row0 + r >= a.rows || n0 + n >= a.n_out) continue;
+    float2 v = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      v.x += part[w][tile][at];
+      v.y += part[w][tile][at + 1];
+    }
+    *(uint32_t*)y_at(a, row0 + r, n0 + n) = pack_bf16(v.x, v.y);
+  }
+}
+
+// ---- more rows: the matrix rate is the bound.  A workgroup takes 128 rows and 128 outputs, a group of 128 channels at a time; a
+// wavefront takes all rows and 32 of the outputs, so that no code is expanded twice in a workgroup.  x goes through registers into LDS,
+// where its words change into the codes' order and its sums over the group are formed; the codes come straight from memory.
+// The sums' part of an output, (z - 16 s) sum x, is a 32x32x16 product of its own for each group: a row's sum as three bf16 numbers
+// (24 bits of it), and 16 times them, against z and -s.
+constexpr int kQTile = 128;
+constexpr int kQStage = kQTile * 256 + kQTile * 16;      // x of a group, then 8 numbers of each row's sum
+constexpr int kQLds = 2 * kQStage + 16;                  // and 16 bytes of zeros
+
+__global__ __launch_bounds__(256, 2) void linear_tile_kernel(LinearArgs a, int row_tiles) {
+  typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+  __shared__ __attribute__((aligned(1024))) char lds_raw[kQLds];
+  lds_char* const lds = (lds_char*)lds_raw;
+  const int lane = lane_id(), wave = wave_id(), tid = threadIdx.x, hl = lane >> 5, col = lane & 31, groups = a.n_in / kQGroup;
+  // neighbours on an XCD share the outputs and take the row tiles in turn
+  const int per = (gridDim.x + 7) / 8, at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  const int row0 = at % row_tiles * kQTile, n0 = at / row_tiles * kQTile;
+  if (n0 >= a.n_out) return;
+  const int n = n0 + 32 * wave + col, nc = n < a.n_out ? n : a.n_out - 1;
+  const char* const codes = a.codes + (int64_t)nc * (a.n_in / 2) + 32 * hl;
+  const uint16_t* const sp = a.scales + (int64_t)nc * groups;
+  const uint16_t* const zp = a.zeros + (int64_t)nc * groups;
+
+  // x: 16 lanes a row, rows 16 i + tid / 16
+  u32x4 xr[8];
+  auto fetch = [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = row0 + 16 * i + (tid >> 4);
+      xr[i] = *(const u32x4*)(x_group(a, r < a.rows ? r : a.rows - 1, g) + 8 * (tid & 15));
+    }
+  };
+  auto settle = [&](int stage) __attribute__((always_inline)) {
+    lds_char* const to = lds + stage * kQStage;
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = 16 * i + (tid >> 4);
+      *(lds_u32x4*)(to + r * 256 + (((tid & 15) ^ (r & 15)) << 4)) = in_code_order(xr[i]);
+      float x = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x += __uint_as_float(xr[i][j] << 16) + __uint_as_float(xr[i][j] & 0xFFFF0000u);
+      x += row_ror<8>(x);
+      x += row_ror<4>(x);
+      x += row_ror<2>(x);
+      sum[i] = x + row_ror<1>(x);
+    }
+    const int c = tid & 15;
+    float x = sum[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) x = (c & 7) == i ? sum[i] : x;
+    const float h = bf16_bits_to_float((uint16_t)pack_bf16(x, 0.f)), m = bf16_bits_to_float((uint16_t)pack_bf16(x - h, 0.f)), l = x - h - m;
+    if (c < 8)
+      *(lds_u32x4*)(to + kQTile * 256 + (16 * c + (tid >> 4)) * 16) = (u32x4){pack_bf16(h, m), pack_bf16(l, 16.f * h), pack_bf16(16.f * m, 16.f * l), 0u};
+  };
+  if (tid == 0) *(lds_u32x4*)(lds + 2 * kQStage) = (u32x4){0, 0, 0, 0};
+  u32x4 w[2], wn[2];
+  uint32_t s16, z16, s16n = 0, z16n = 0;
+  fetch(0);
+  w[0] = *(const u32x4*)codes;
+  w[1] = *(const u32x4*)(codes + 16);
+  s16 = sp[0];
+  z16 = zp[0];
+  wn[0] = w[0];
+  wn[1] = w[1];
+  settle(0);
+
+  uint32_t off[8];                              // x operand of channels 64 hl + 8 k ..
+#pragma unroll
+  for (int k = 0; k < 8; ++k) off[k] = (uint32_t)(col * 256 + (((8 * hl + k) ^ (col & 15)) << 4));
+  f32x16 y[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) y[t][r] = 0.f;
+  for (int g = 0; g < groups; ++g) {
+    const int stage = g & 1;
+    __syncthreads();
+    if (g + 1 < groups) {
+      fetch(g + 1);
+      wn[0] = *(const u32x4*)(codes + (int64_t)(g + 1) * 64);
+      wn[1] = *(const u32x4*)(codes + (int64_t)(g + 1) * 64 + 16);
+      s16n = sp[g + 1];
+      z16n = zp[g + 1];
+    }
+    lds_char* const xt = lds + stage * kQStage;
+    f32x16 acc[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const bf16x8 b = codes_to_bf16(w[k >> 2][k & 3]);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read16(xt + off[k] + t * 8192), b, acc[t], 0, 0, 0);
+    }
+    const uint32_t minus_s = s16 ^ 0x8000u;
+    const bf16x8 zs = __builtin_bit_cast(bf16x8, hl ? (u32x4){0, 0, 0, 0} : (u32x4){z16 | (z16 << 16), z16 | (minus_s << 16), minus_s | (minus_s << 16), 0u});
+    const float s = __uint_as_float(s16 << 16);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      y[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read16(hl ? lds + 2 * kQStage : xt + kQTile * 256 + (32 * t + col) * 16), zs, y[t], 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) y[t][r] = __builtin_fmaf(s, acc[t][r], y[t][r]);
+    }
+    if (g + 1 < groups) settle(1 - stage);
+    w[0] = wn[0];
+    w[1] = wn[1];
+    s16 = s16n;
+    z16 = z16n;
+  }
+  if (n >= a.n_out) return;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int row = row0 + 32 * t + 8 * (r >> 2) + 4 * hl + (r & 3);
+      if (row < a.rows) *y_at(a, row, n) = (uint16_t)pack_bf16(y[t][r], 0.f);
+    }
+}
+
+template <int RT, int NT, int U>
+void few_go(hipStream_t s, const LinearArgs& a) {
+  hipLaunchKernelGGL((linear_few_kernel<RT, NT, U>), dim3((unsigned)ceil_div(a.n_out, 16 * NT), (unsigned)ceil_div(a.rows, 16 * RT)), dim3(512), 0, s, a);
 }
 
 }  // namespace
@@ -132,7 +379,17 @@ extern "C" hi_status hi_linear_quantized(void* stream, const void* x_dev, const 
   StreamDevice on(stream);
   const LinearArgs a = {(const uint16_t*)x_dev, (const char*)codes_dev, (const uint16_t*)scales_dev, (const uint16_t*)zeros_dev,
                         (uint16_t*)y_dev, n_rows, n_in, n_out, x_heads, y_heads};
-  hipLaunchKernelGGL(linear_simple_kernel, dim3((unsigned)n_out, (unsigned)(n_rows < 32768 ? n_rows : 32768)), dim3(64), 0,
-                     (hipStream_t)stream, a);
+  const hipStream_t st = (hipStream_t)stream;
+  if (n_rows <= 16) {
+    few_go<1, 1, 4>(st, a);
+  } else if (n_rows <= 32) {
+    few_go<2, 2, 2>(st, a);
+  } else if (n_rows <= 64) {
+    few_go<4, 2, 1>(st, a);
+  } else {
+    const int64_t row_tiles = ceil_div(n_rows, kQTile), tiles = row_tiles * ceil_div(n_out, kQTile);
+    if (tiles > 0x7FFFFFF0) { set_last_error("quantised linear: too many rows"); return HI_ERR_RANGE; }
+    hipLaunchKernelGGL(linear_tile_kernel, dim3((unsigned)(8 * ceil_div(tiles, 8))), dim3(256), 0, st, a, (int)row_tiles);
+  }
   return launched("quantised linear");
 }

@@ -1,4 +1,5 @@
 // Products with weights of 4 bits: W^ [n_out][n_in] = zero + code * scale, a scale and a zero for each 128 input channels of a row.
+#include <mutex>
 #include "hi_device.h"
 #include "hi_serve.h"
 
@@ -7,6 +8,7 @@ namespace hi {
 namespace {
 
 constexpr int kQGroup = 128;                    // input channels of a scale
+constexpr int kQMostIn = 1 << 20;               // 64 rows of x, or 16 of codes, within 32 bits of bytes
 
 // ---- bf16 weights to codes: a wavefront takes 16 groups at a time, 4 lanes a group with 32 channels each.  The weights are read
 // once and a quarter of them written; run once per matrix.
@@ -101,109 +103,171 @@ __device__ __forceinline__ uint16_t* y_at(const LinearArgs& a, int row, int n) {
   return a.y + (a.y_heads ? ((int64_t)(n >> 7) * a.rows + row) * kHeadDim + (n & 127) : (int64_t)row * a.n_out + n);
 }
 
-// ---- up to 64 rows: the read of the weights is the bound.  A workgroup takes 16 NT outputs and all rows (RT tiles of 16); its 8
-// wavefronts take the groups in turn and add their sums through LDS.  A lane reads 32 consecutive codes of its output, and the same
-// 32 channels of its row of x; U groups are under way at a time.  Sums of x come out of the matrix pipe too, against ones.
-template <int RT, int NT, int U>
-__global__ __launch_bounds__(512, RT == 1 ? 4 : 2) void linear_few_kernel(LinearArgs a) {
-  __shared__ float part[8][RT * NT][256];
+// ---- up to 64 rows: the read of the weights is the bound.  A workgroup takes 16 NT outputs and all rows (4 RX of them); its W
+// wavefronts take turns of U consecutive groups each and add their sums through LDS.  Codes and x come through a private LDS ring of S
+// groups a wavefront, by direct loads: as the matrix tiles want them, 16 neighbouring lanes would touch 16 rows, and the look-up of
+// their lines, not the bytes, would be the bound (16 rows of 4096 x 6144: 13.0 us with loads into registers).  Sums of x come
+// out of the matrix pipe too, against ones.
+// A workgroup begins its turns where its number says: the rows of codes lie a power of two apart, and workgroups that all began at
+// the first channel would keep to a few memory channels.
+template <int RX, int NT, int U, int W, int S>
+struct Few {
+  static constexpr int kTiles = RX < 4 ? 1 : RX / 4, kLoads = RX + NT, kStage = kLoads * 1024;
+  static constexpr int kRing = W * S * kStage, kSums = W * kTiles * NT * 1024, kLds = kRing > kSums ? kRing : kSums;
+  static constexpr int kPerSimd = kLds <= 80 * 1024 ? W / 2 : W / 4;          // wavefronts on a SIMD, by LDS
+};
+
+template <int RX, int NT, int U, int W, int S>
+__global__ __launch_bounds__(64 * W, (Few<RX, NT, U, W, S>::kPerSimd)) void linear_few_kernel(LinearArgs a) {
+  using F = Few<RX, NT, U, W, S>;
+  constexpr int RT = F::kTiles;
+  static_assert((S - 1) * F::kLoads < 64 && F::kLds <= 160 * 1024, "ring");
+  extern __shared__ __attribute__((aligned(1024))) char lds_raw[];
   const int lane = lane_id(), wave = wave_id(), c16 = lane & 15, g4 = lane >> 4;
-  const int n0 = blockIdx.x * 16 * NT, row0 = blockIdx.y * 16 * RT, groups = a.n_in / kQGroup;
+  const int n0 = blockIdx.x * 16 * NT, row0 = blockIdx.y * 4 * RX, groups = a.n_in / kQGroup;
+  const int turns = (groups + U - 1) / U, begin = blockIdx.x % turns;
+  const uint32_t ring = (uint32_t)(uintptr_t)(lds_char*)lds_raw + wave * (S * F::kStage);
+
+  // a load of codes: 4 lanes an output, 16 outputs (chunk p of output r of the tile is chunk p ^ (r / 4) of its 64 bytes)
+  const int cr = lane >> 2;
+  const uint32_t code_off = (uint32_t)cr * (uint32_t)(a.n_in / 2) + ((((uint32_t)lane & 3) ^ ((uint32_t)cr >> 2)) << 4);
   const char* codes[NT];
   const uint16_t *sp[NT], *zp[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int n = n0 + 16 * t + c16 < a.n_out ? n0 + 16 * t + c16 : a.n_out - 1;
-    codes[t] = a.codes + (int64_t)n * (a.n_in / 2) + 16 * g4;
-    sp[t] = a.scales + (int64_t)n * groups;
-    zp[t] = a.zeros + (int64_t)n * groups;
+    const int n = n0 + 16 * t < a.n_out ? n0 + 16 * t : n0;           // (a tile of outputs is there or not)
+    codes[t] = a.codes + (int64_t)n * (a.n_in / 2);
+    sp[t] = a.scales + (int64_t)(n + c16) * groups;
+    zp[t] = a.zeros + (int64_t)(n + c16) * groups;
   }
-  int row[RT];
+  // a load of x: 16 lanes a row, 4 rows (chunk p of row r is chunk p ^ (r % 16) of its 256 bytes)
+  uint32_t x_off[RX];
+  const uint32_t pitch = a.x_heads ? 2 * kQGroup : 2u * a.n_in;
 #pragma unroll
-  for (int t = 0; t < RT; ++t) row[t] = row0 + 16 * t + c16 < a.rows ? row0 + 16 * t + c16 : a.rows - 1;
+  for (int i = 0; i < RX; ++i) {
+    const int r = 4 * i + (lane >> 4), to = row0 + r < a.rows ? r : a.rows - 1 - row0;
+    x_off[i] = (uint32_t)to * pitch + (uint32_t)(((lane & 15) ^ (r & 15)) << 4);
+  }
+  const char* const x0 = (const char*)a.x + (int64_t)row0 * pitch;
+  const int64_t x_group_bytes = a.x_heads ? (int64_t)a.rows * (2 * kQGroup) : 2 * kQGroup;
+
+  const int mine = turns > wave ? (turns - wave + W - 1) / W : 0;     // turns of this wavefront: wave, wave + W, ..
+  auto first_group = [&](int i) __attribute__((always_inline)) {
+    const int turn = wave + W * i + begin;
+    return (turn < turns ? turn : turn - turns) * U;
+  };
+  auto issue = [&](int step, int stage) __attribute__((always_inline)) {      // step: turn and group of it, one after the other
+    int g = first_group(step / U) + step % U;
+    g = g < groups ? g : groups - 1;                                  // (of a turn that is cut short: loaded, and not used)
+    const uint32_t to = ring + stage * F::kStage;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) g2lds16_s<0>(codes[t] + (int64_t)g * (kQGroup / 2), code_off, to + t * 1024);
+#pragma unroll
+    for (int i = 0; i < RX; ++i) g2lds16_s<0>(x0 + g * x_group_bytes, x_off[i], to + (NT + i) * 1024);
+  };
+  struct Scales { uint16_t s[NT][U], z[NT][U]; };
+  auto load_scales = [&](Scales& b, int g) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      if (g + U <= groups) {                     // (2-byte aligned: the hardware takes it in one piece all the same)
+        __builtin_memcpy(b.s[t], sp[t] + g, 2 * U);
+        __builtin_memcpy(b.z[t], zp[t] + g, 2 * U);
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          b.s[t][u] = g + u < groups ? sp[t][g + u] : 0;
+          b.z[t][u] = g + u < groups ? zp[t][g + u] : 0;
+        }
+      }
+    }
+  };
+  Scales now, next;
+  if (mine > 0) load_scales(now, first_group(0));
+  for (int i = 0; i < S - 1; ++i)
+    if (i < mine * U) issue(i, i);
+
+  uint32_t x_at[4];                              // operand reads: row c16 of a tile, channels 32 g4 + 8 k ..
+  const int rr = RX < 4 ? c16 & (4 * RX - 1) : c16;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x_at[k] = (uint32_t)(NT * 1024 + rr * 256 + (((4 * g4 + k) ^ rr) << 4));
+  const uint32_t w_at = (uint32_t)(c16 * 64 + ((g4 ^ (c16 >> 2)) << 4));
   f32x4 y[RT][NT];
 #pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll
     for (int t = 0; t < NT; ++t) y[i][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-  struct Group {
-    u32x4 w[NT], x[RT][4];
-    uint16_t s[NT], z[NT];
-  };
-  auto load = [&](Group& b, int g) __attribute__((always_inline)) {
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      b.w[t] = __builtin_nontemporal_load((const u32x4*)(codes[t] + (int64_t)g * (kQGroup / 2)));
-      b.s[t] = sp[t][g];
-      b.z[t] = zp[t][g];
-    }
-#pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      const uint16_t* const x = x_group(a, row[i], g) + 32 * g4;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) b.x[i][k] = *(const u32x4*)(x + 8 * k);
-    }
-  };
-  auto add = [&](const Group& b) __attribute__((always_inline)) {
-    f32x4 acc[RT][NT], xs[RT];
-#pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      xs[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int t = 0; t < NT; ++t) acc[i][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      bf16x8 w[NT];
-#pragma unroll
-      for (int t = 0; t < NT; ++t) w[t] = codes_to_bf16(b.w[t][k]);
-#pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        const bf16x8 x = __builtin_bit_cast(bf16x8, in_code_order(b.x[i][k]));
-        xs[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, bf16_ones(), xs[i], 0, 0, 0);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w[t], acc[i][t], 0, 0, 0);
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const float s = bf16_bits_to_float(b.s[t]), z = __builtin_fmaf(-16.0f, s, bf16_bits_to_float(b.z[t]));
-#pragma unroll
-      for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) y[i][t][r] = __builtin_fmaf(s, acc[i][t][r], __builtin_fmaf(z, xs[i][r], y[i][t][r]));
-    }
-  };
-  Group b[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (wave + 8 * u < groups) load(b[u], wave + 8 * u);
-  for (int g = wave; g < groups; g += 8 * U) {
+  int stage = 0, ahead = S - 1;
+  for (int turn = 0; turn < mine; ++turn) {
+    const int g = first_group(turn);
+    if (turn + 1 < mine) load_scales(next, first_group(turn + 1));
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int at = g + 8 * u;
-      if (at < groups) {
-        add(b[u]);
-        if (at + 8 * U < groups) load(b[u], at + 8 * U);
+      const int step = turn * U + u;
+      if (step + S - 1 < mine * U) {
+        issue(step + S - 1, ahead);
+        wait_vmcnt<(S - 1) * F::kLoads>();
+      } else {
+        wait_vmcnt<0>();
       }
+      lds_char* const at = (lds_char*)(uintptr_t)(ring + stage * F::kStage);
+      if (g + u < groups) {
+        u32x4 w[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) w[t] = __builtin_bit_cast(u32x4, lds_read16(at + w_at + t * 1024));
+        f32x4 acc[RT][NT], xs[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+          xs[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int t = 0; t < NT; ++t) acc[i][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          bf16x8 wk[NT];
+#pragma unroll
+          for (int t = 0; t < NT; ++t) wk[t] = codes_to_bf16(w[t][k]);
+#pragma unroll
+          for (int i = 0; i < RT; ++i) {
+            const bf16x8 x = __builtin_bit_cast(bf16x8, in_code_order(__builtin_bit_cast(u32x4, lds_read16(at + x_at[k] + i * 4096))));
+            xs[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, bf16_ones(), xs[i], 0, 0, 0);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, wk[t], acc[i][t], 0, 0, 0);
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const float s = bf16_bits_to_float(now.s[t][u]), z = __builtin_fmaf(-16.0f, s, bf16_bits_to_float(now.z[t][u]));
+#pragma unroll
+          for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[i][t][r] = __builtin_fmaf(s, acc[i][t][r], __builtin_fmaf(z, xs[i][r], y[i][t][r]));
+        }
+      }
+      asm volatile("" ::: "memory");
+      stage = stage + 1 < S ? stage + 1 : 0;
+      ahead = ahead + 1 < S ? ahead + 1 : 0;
     }
+    now = next;
   }
   // register r: row 4 g4 + r of the tile, output c16
+  float* const part = (float*)lds_raw;           // [wavefront][tile][16 rows][16 outputs]
+  __syncthreads();
 #pragma unroll
   for (int i = 0; i < RT; ++i)
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) part[wave][i * NT + t][(4 * g4 + r) * 16 + c16] = y[i][t][r];
+      for (int r = 0; r < 4; ++r) part[(wave * RT * NT + i * NT + t) * 256 + (4 * g4 + r) * 16 + c16] = y[i][t][r];
   __syncthreads();
-  for (int i = threadIdx.x; i < RT * NT * 128; i += 512) {          // two outputs of a row each
-    const int n = 2 * (i % (8 * NT)), r = i / (8 * NT), tile = (r >> 4) * NT + (n >> 4), at = (r & 15) * 16 + (n & 15);
+  for (int i = threadIdx.x; i < 4 * RX * NT * 8; i += 64 * W) {       // two outputs of a row each
+    const int n = 2 * (i % (8 * NT)), r = i / (8 * NT), at = ((r >> 4) * NT + (n >> 4)) * 256 + (r & 15) * 16 + (n & 15);
     if (row0 + r >= a.rows || n0 + n >= a.n_out) continue;
     float2 v = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int w = 0; w < 8; ++w) {
-      v.x += part[w][tile][at];
-      v.y += part[w][tile][at + 1];
+    for (int w = 0; w < W; ++w) {
+      const float2 x = *(const float2*)(part + w * RT * NT * 256 + at);
+      v.x += x.x;
+      v.y += x.y;
     }
     *(uint32_t*)y_at(a, row0 + r, n0 + n) = pack_bf16(v.x, v.y);
   }
@@ -331,9 +395,22 @@ __global__ __launch_bounds__(256, 2) void linear_tile_kernel(LinearArgs a, int r
     }
 }
 
-template <int RT, int NT, int U>
-void few_go(hipStream_t s, const LinearArgs& a) {
-  hipLaunchKernelGGL((linear_few_kernel<RT, NT, U>), dim3((unsigned)ceil_div(a.n_out, 16 * NT), (unsigned)ceil_div(a.rows, 16 * RT)), dim3(512), 0, s, a);
+template <int RX, int NT, int U, int W, int S>
+hipError_t few_go(hipStream_t s, const LinearArgs& a) {
+  using F = Few<RX, NT, U, W, S>;
+  static std::once_flag once;
+  static hipError_t attr = hipSuccess;
+  std::call_once(once, [] { attr = hipFuncSetAttribute((const void*)linear_few_kernel<RX, NT, U, W, S>, hipFuncAttributeMaxDynamicSharedMemorySize, F::kLds); });
+  if (attr != hipSuccess) return attr;
+  hipLaunchKernelGGL((linear_few_kernel<RX, NT, U, W, S>), dim3((unsigned)ceil_div(a.n_out, 16 * NT), (unsigned)ceil_div(a.rows, 4 * RX)), dim3(64 * W),
+                     F::kLds, s, a);
+  return hipSuccess;
+}
+// turns of 4 groups, as long as each wavefront has one
+template <int RX, int NT, int W, int S>
+hipError_t few_turns(hipStream_t s, const LinearArgs& a) {
+  const int groups = a.n_in / kQGroup;
+  return groups >= 4 * W ? few_go<RX, NT, 4, W, S>(s, a) : groups >= 2 * W ? few_go<RX, NT, 2, W, S>(s, a) : few_go<RX, NT, 1, W, S>(s, a);
 }
 
 }  // namespace
@@ -375,21 +452,23 @@ extern "C" hi_status hi_linear_quantized(void* stream, const void* x_dev, const 
     set_last_error("quantised linear: n_in must be a multiple of %d, n_out of 16, and of %d for head-major outputs", kQGroup, kHeadDim);
     return HI_ERR_UNSUPPORTED;
   }
+  if (n_in > kQMostIn) { set_last_error("quantised linear: n_in of more than %d", kQMostIn); return HI_ERR_UNSUPPORTED; }
   if (n_rows == 0) return HI_OK;
   StreamDevice on(stream);
   const LinearArgs a = {(const uint16_t*)x_dev, (const char*)codes_dev, (const uint16_t*)scales_dev, (const uint16_t*)zeros_dev,
                         (uint16_t*)y_dev, n_rows, n_in, n_out, x_heads, y_heads};
   const hipStream_t st = (hipStream_t)stream;
-  if (n_rows <= 16) {
-    few_go<1, 1, 4>(st, a);
-  } else if (n_rows <= 32) {
-    few_go<2, 2, 2>(st, a);
-  } else if (n_rows <= 64) {
-    few_go<4, 2, 1>(st, a);
-  } else {
+  hipError_t e = hipSuccess;
+  if (n_rows <= 4) e = few_turns<1, 1, 8, 4>(st, a);
+  else if (n_rows <= 8) e = few_turns<2, 1, 8, 3>(st, a);
+  else if (n_rows <= 16) e = few_turns<4, 1, 8, 2>(st, a);
+  else if (n_rows <= 32) e = few_turns<8, 2, 8, 2>(st, a);
+  else if (n_rows <= 64) e = few_turns<16, 2, 4, 2>(st, a);
+  else {
     const int64_t row_tiles = ceil_div(n_rows, kQTile), tiles = row_tiles * ceil_div(n_out, kQTile);
     if (tiles > 0x7FFFFFF0) { set_last_error("quantised linear: too many rows"); return HI_ERR_RANGE; }
     hipLaunchKernelGGL(linear_tile_kernel, dim3((unsigned)(8 * ceil_div(tiles, 8))), dim3(256), 0, st, a, (int)row_tiles);
   }
+  if (e != hipSuccess) { set_last_error("quantised linear: %s", hipGetErrorString(e)); return HI_ERR_HIP; }
   return launched("quantised linear");
 }

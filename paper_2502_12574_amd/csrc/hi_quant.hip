@@ -1,5 +1,6 @@
 // Products with weights of 4 bits: W^ [n_out][n_in] = zero + code * scale, a scale and a zero for each 128 input channels of a row.
 #include <mutex>
+#include <type_traits>
 #include "hi_device.h"
 #include "hi_serve.h"
 
@@ -72,26 +73,29 @@ struct LinearArgs {
   int rows, n_in, n_out, x_heads, y_heads;
 };
 
-// A code c becomes the bf16 number 16 + c with two operations for two codes: 16 .. 31 is an exponent and the code in the upper bits of
-// the fraction.  So with s and z a group's scale and zero, and exactly in all but the fp32 sums,
+// A code c becomes the bf16 number 16 + c: 16 .. 31 is an exponent and the code in the upper bits of the fraction.  So with s and z a
+// group's scale and zero, and exactly in all but the fp32 sums,
 //   sum_k W^_k x_k = s sum_k (16 + c_k) x_k + (z - 16 s) sum_k x_k   over the group's 128 channels:
 // no weight is rounded, and scale and zero enter once a group instead of once a weight.
-// A word holds the codes of 8 channels; the pairs come out as (0, 4), (1, 5), (2, 6), (3, 7), an order that x is brought into.
-__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t w) {
-  u32x4 b;
-  b[0] = ((w << 3) & 0x00780078u) | 0x41804180u;
-  b[1] = ((w >> 1) & 0x00780078u) | 0x41804180u;
-  b[2] = ((w >> 5) & 0x00780078u) | 0x41804180u;
-  b[3] = ((w >> 9) & 0x00780078u) | 0x41804180u;
-  return __builtin_bit_cast(bf16x8, b);
+// A byte holds two codes, which belong 12 bits further apart: a product with 2^3 + 2^15 puts both where they have to be, among others
+// that the mask takes out.  Two operations for two codes (with shifts, too, but those pair codes that are 4 channels apart, and x had
+// to be brought into that order).  The constants are kept in registers: such an instruction cannot carry them.
+struct CodeBits {
+  uint32_t spread = 0x8008u, mask = 0x00780078u, one = 0x41804180u;
+  __device__ __forceinline__ CodeBits() { asm("" : "+v"(spread), "+s"(mask), "+v"(one)); }
+};
+template <int BYTE>
+__device__ __forceinline__ uint32_t codes_pair(uint32_t w, const CodeBits& c) {
+  static_assert(BYTE >= 0 && BYTE < 4, "a byte of a word");
+  uint32_t x;
+  if constexpr (BYTE == 0) asm("v_mul_u32_u24_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0 src1_sel:DWORD" : "=v"(x) : "v"(w), "v"(c.spread));
+  else if constexpr (BYTE == 1) asm("v_mul_u32_u24_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1 src1_sel:DWORD" : "=v"(x) : "v"(w), "v"(c.spread));
+  else if constexpr (BYTE == 2) asm("v_mul_u32_u24_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2 src1_sel:DWORD" : "=v"(x) : "v"(w), "v"(c.spread));
+  else asm("v_mul_u32_u24_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3 src1_sel:DWORD" : "=v"(x) : "v"(w), "v"(c.spread));
+  return (x & c.mask) | c.one;
 }
-__device__ __forceinline__ u32x4 in_code_order(u32x4 x) {
-  u32x4 y;
-  y[0] = __builtin_amdgcn_perm(x[2], x[0], 0x05040100);
-  y[1] = __builtin_amdgcn_perm(x[2], x[0], 0x07060302);
-  y[2] = __builtin_amdgcn_perm(x[3], x[1], 0x05040100);
-  y[3] = __builtin_amdgcn_perm(x[3], x[1], 0x07060302);
-  return y;
+__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t w, const CodeBits& c) {
+  return __builtin_bit_cast(bf16x8, (u32x4){codes_pair<0>(w, c), codes_pair<1>(w, c), codes_pair<2>(w, c), codes_pair<3>(w, c)});
 }
 __device__ __forceinline__ bf16x8 bf16_ones() { return __builtin_bit_cast(bf16x8, (u32x4){0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}); }
 
@@ -196,6 +200,7 @@ __global__ __launch_bounds__(64 * W, (Few<RX, NT, U, W, S>::kPerSimd)) void line
   for (int i = 0; i < RT; ++i)
 #pragma unroll
     for (int t = 0; t < NT; ++t) y[i][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  const CodeBits bits;
   int stage = 0, ahead = S - 1;
   for (int turn = 0; turn < mine; ++turn) {
     const int g = first_group(turn);
@@ -225,10 +230,10 @@ __global__ __launch_bounds__(64 * W, (Few<RX, NT, U, W, S>::kPerSimd)) void line
         for (int k = 0; k < 4; ++k) {
           bf16x8 wk[NT];
 #pragma unroll
-          for (int t = 0; t < NT; ++t) wk[t] = codes_to_bf16(w[t][k]);
+          for (int t = 0; t < NT; ++t) wk[t] = codes_to_bf16(w[t][k], bits);
 #pragma unroll
           for (int i = 0; i < RT; ++i) {
-            const bf16x8 x = __builtin_bit_cast(bf16x8, in_code_order(__builtin_bit_cast(u32x4, lds_read16(at + x_at[k] + i * 4096))));
+            const bf16x8 x = lds_read16(at + x_at[k] + i * 4096);
             xs[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, bf16_ones(), xs[i], 0, 0, 0);
 #pragma unroll
             for (int t = 0; t < NT; ++t) acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, wk[t], acc[i][t], 0, 0, 0);
@@ -274,19 +279,24 @@ __global__ __launch_bounds__(64 * W, (Few<RX, NT, U, W, S>::kPerSimd)) void line
 }
 
 // ---- more rows: the matrix rate is the bound.  A workgroup takes 128 rows and 128 outputs, a group of 128 channels at a time; a
-// wavefront takes all rows and 32 of the outputs, so that no code is expanded twice in a workgroup.  x goes through registers into LDS,
-// where its words change into the codes' order and its sums over the group are formed; the codes come straight from memory.
+// wavefront takes all rows and 32 of the outputs, so that no code is expanded twice in a workgroup.  x goes to LDS by direct loads, a
+// step ahead, the codes into registers.  Operands are read four ahead of the products that take them (left to itself the compiler reads
+// each where it is needed, and the products wait for LDS: 4096 x 4096 and 1500 rows 101 us).
 // The sums' part of an output, (z - 16 s) sum x, is a 32x32x16 product of its own for each group: a row's sum as three bf16 numbers
-// (24 bits of it), and 16 times them, against z and -s.
+// (24 bits of it), and 16 times them, against z and -s.  Each wavefront forms the sums of 32 rows, from the operands that it reads
+// anyway, for all four; they are used a step later.
 constexpr int kQTile = 128;
-constexpr int kQStage = kQTile * 256 + kQTile * 16;      // x of a group, then 8 numbers of each row's sum
-constexpr int kQLds = 2 * kQStage + 16;                  // and 16 bytes of zeros
+constexpr int kQStage = kQTile * 256;                    // x of a group
+constexpr int kQSums = 2 * kQStage;                      // [stage][row] 8 numbers of a row's sum, then 16 bytes of zeros
+constexpr int kQZeros = kQSums + 2 * kQTile * 16;
+constexpr int kQLds = kQZeros + 16;
 
 __global__ __launch_bounds__(256, 2) void linear_tile_kernel(LinearArgs a, int row_tiles) {
   typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
   __shared__ __attribute__((aligned(1024))) char lds_raw[kQLds];
   lds_char* const lds = (lds_char*)lds_raw;
-  const int lane = lane_id(), wave = wave_id(), tid = threadIdx.x, hl = lane >> 5, col = lane & 31, groups = a.n_in / kQGroup;
+  const int lane = lane_id(), wave = wave_id(), hl = lane >> 5, col = lane & 31, groups = a.n_in / kQGroup;
   // neighbours on an XCD share the outputs and take the row tiles in turn
   const int per = (gridDim.x + 7) / 8, at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
   const int row0 = at % row_tiles * kQTile, n0 = at / row_tiles * kQTile;
@@ -296,101 +306,112 @@ __global__ __launch_bounds__(256, 2) void linear_tile_kernel(LinearArgs a, int r
   const uint16_t* const sp = a.scales + (int64_t)nc * groups;
   const uint16_t* const zp = a.zeros + (int64_t)nc * groups;
 
-  // x: 16 lanes a row, rows 16 i + tid / 16
-  u32x4 xr[8];
-  auto fetch = [&](int g) __attribute__((always_inline)) {
+  // x: the wavefront brings rows 32 wave .. of a tile, 4 to a load (chunk p of row r is chunk p ^ (r % 16) of its 256 bytes)
+  const uint32_t pitch = a.x_heads ? 2 * kQGroup : 2u * a.n_in;
+  const char* x_now = (const char*)a.x + (int64_t)row0 * pitch;
+  const int64_t x_step = a.x_heads ? (int64_t)a.rows * (2 * kQGroup) : 2 * kQGroup;
+  const uint32_t lds_wave = (uint32_t)(uintptr_t)lds + wave * 8192;
+  uint32_t x_off[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = row0 + 16 * i + (tid >> 4);
-      xr[i] = *(const u32x4*)(x_group(a, r < a.rows ? r : a.rows - 1, g) + 8 * (tid & 15));
-    }
+  for (int i = 0; i < 8; ++i) {
+    const int r = 32 * wave + 4 * i + (lane >> 4);
+    x_off[i] = (uint32_t)(row0 + r < a.rows ? r : a.rows - 1 - row0) * pitch + (((lane & 15) ^ (r & 15)) << 4);
+  }
+  struct Codes { u32x4 w[2]; uint32_t s, z; };
+  auto fetch = [&](Codes& b, int g, int stage) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g2lds16_s<0>(x_now, x_off[i], lds_wave + stage * kQStage + i * 1024);
+    x_now += x_step;
+    b.w[0] = *(const u32x4*)(codes + (int64_t)g * 64);
+    b.w[1] = *(const u32x4*)(codes + (int64_t)g * 64 + 16);
+    b.s = sp[g];
+    b.z = zp[g];
   };
-  auto settle = [&](int stage) __attribute__((always_inline)) {
-    lds_char* const to = lds + stage * kQStage;
-    float sum[8];
+  if (threadIdx.x == 0) *(lds_u32x4*)(lds + kQZeros) = (u32x4){0, 0, 0, 0};
+  // x operand j of channels 64 hl + 8 k ..: row tile j ^ wave, the wavefront's own first; bits 4 .. 6 change with k
+  uint32_t x_at[4], sum_at[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int r = 16 * i + (tid >> 4);
-      *(lds_u32x4*)(to + r * 256 + (((tid & 15) ^ (r & 15)) << 4)) = in_code_order(xr[i]);
-      float x = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x += __uint_as_float(xr[i][j] << 16) + __uint_as_float(xr[i][j] & 0xFFFF0000u);
-      x += row_ror<8>(x);
-      x += row_ror<4>(x);
-      x += row_ror<2>(x);
-      sum[i] = x + row_ror<1>(x);
-    }
-    const int c = tid & 15;
-    float x = sum[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) x = (c & 7) == i ? sum[i] : x;
-    const float h = bf16_bits_to_float((uint16_t)pack_bf16(x, 0.f)), m = bf16_bits_to_float((uint16_t)pack_bf16(x - h, 0.f)), l = x - h - m;
-    if (c < 8)
-      *(lds_u32x4*)(to + kQTile * 256 + (16 * c + (tid >> 4)) * 16) = (u32x4){pack_bf16(h, m), pack_bf16(l, 16.f * h), pack_bf16(16.f * m, 16.f * l), 0u};
-  };
-  if (tid == 0) *(lds_u32x4*)(lds + 2 * kQStage) = (u32x4){0, 0, 0, 0};
-  u32x4 w[2], wn[2];
-  uint32_t s16, z16, s16n = 0, z16n = 0;
-  fetch(0);
-  w[0] = *(const u32x4*)codes;
-  w[1] = *(const u32x4*)(codes + 16);
-  s16 = sp[0];
-  z16 = zp[0];
-  wn[0] = w[0];
-  wn[1] = w[1];
-  settle(0);
-
-  uint32_t off[8];                              // x operand of channels 64 hl + 8 k ..
-#pragma unroll
-  for (int k = 0; k < 8; ++k) off[k] = (uint32_t)(col * 256 + (((8 * hl + k) ^ (col & 15)) << 4));
+  for (int j = 0; j < 4; ++j) {
+    x_at[j] = (uint32_t)(((j ^ wave) * 32 + col) * 256 + (((8 * hl) ^ (col & 15)) << 4));
+    sum_at[j] = hl ? kQZeros : kQSums + ((j ^ wave) * 32 + col) * 16;
+  }
+  const uint32_t my_sum = kQSums + (wave * 32 + col) * 16;
   f32x16 y[4];
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) y[t][r] = 0.f;
-  for (int g = 0; g < groups; ++g) {
-    const int stage = g & 1;
+  const CodeBits bits;
+  u32x4 zs = {0, 0, 0, 0};                       // the last step's z and -s
+  auto add_sums = [&](int stage) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read16(lds + sum_at[j] + (hl ? 0 : stage * (kQTile * 16))), __builtin_bit_cast(bf16x8, zs), y[j], 0, 0, 0);
+  };
+  auto step = [&](int g, auto parity, Codes& now, Codes& next) __attribute__((always_inline)) {
+    constexpr int stage = decltype(parity)::value, A = 4;
+    wait_vmcnt<0>();
+    asm volatile("" : "+v"(now.w[0]), "+v"(now.w[1]), "+v"(now.s), "+v"(now.z));      // (they were asked for a step ago)
     __syncthreads();
-    if (g + 1 < groups) {
-      fetch(g + 1);
-      wn[0] = *(const u32x4*)(codes + (int64_t)(g + 1) * 64);
-      wn[1] = *(const u32x4*)(codes + (int64_t)(g + 1) * 64 + 16);
-      s16n = sp[g + 1];
-      z16n = zp[g + 1];
-    }
+    if (g + 1 < groups) fetch(next, g + 1, 1 - stage);
     lds_char* const xt = lds + stage * kQStage;
     f32x16 acc[4];
+    bf16x8 op[A + 1], b[2];
+    float sum = 0.f;
+    auto read = [&](int i) __attribute__((always_inline)) { op[i % (A + 1)] = lds_read16(xt + (x_at[i & 3] ^ ((i >> 2) << 4))); };
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int i = 0; i < A; ++i) read(i);
+    b[0] = codes_to_bf16(now.w[0][0], bits);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[t][r] = 0.f;
+    for (int i = 0; i < 32; ++i) {
+      const int k = i >> 2, j = i & 3;
+      if (i + A < 32) read(i + A);
+      f32x16 z;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const bf16x8 b = codes_to_bf16(w[k >> 2][k & 3]);
+      for (int r = 0; r < 16; ++r) z[r] = 0.f;
+      acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i % (A + 1)], b[k & 1], k == 0 ? z : acc[j], 0, 0, 0);
+      if (j == 0) {                              // the own rows' sums
+        const u32x4 x = __builtin_bit_cast(u32x4, op[i % (A + 1)]);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read16(xt + off[k] + t * 8192), b, acc[t], 0, 0, 0);
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t two = x[q];             // (a vector's element itself would be cast as the vector's first)
+          sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
+        }
+        asm volatile("" : "+v"(sum));            // here, and not where it is used: the operands would be kept until then
+      }
+      if (j == 1 && k < 7) b[(k + 1) & 1] = codes_to_bf16(now.w[(k + 1) >> 2][(k + 1) & 3], bits);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    const uint32_t minus_s = s16 ^ 0x8000u;
-    const bf16x8 zs = __builtin_bit_cast(bf16x8, hl ? (u32x4){0, 0, 0, 0} : (u32x4){z16 | (z16 << 16), z16 | (minus_s << 16), minus_s | (minus_s << 16), 0u});
-    const float s = __uint_as_float(s16 << 16);
+    if (g > 0) add_sums(1 - stage);              // of the step before
+    const uint32_t minus_s = now.s ^ 0x8000u;
+    zs = (u32x4){hl ? 0 : now.z | (now.z << 16), hl ? 0 : now.z | (minus_s << 16), hl ? 0 : minus_s | (minus_s << 16), 0u};
+    const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+    sum = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
+    const float h = bf16_bits_to_float((uint16_t)pack_bf16(sum, 0.f)), m = bf16_bits_to_float((uint16_t)pack_bf16(sum - h, 0.f)), l = sum - h - m;
+    *(lds_u32x4*)(lds + my_sum + stage * (kQTile * 16)) = (u32x4){pack_bf16(h, m), pack_bf16(l, 16.f * h), pack_bf16(16.f * m, 16.f * l), 0u};
+    const float s = __uint_as_float(now.s << 16);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      y[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read16(hl ? lds + 2 * kQStage : xt + kQTile * 256 + (32 * t + col) * 16), zs, y[t], 0, 0, 0);
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) y[t][r] = __builtin_fmaf(s, acc[t][r], y[t][r]);
-    }
-    if (g + 1 < groups) settle(1 - stage);
-    w[0] = wn[0];
-    w[1] = wn[1];
-    s16 = s16n;
-    z16 = z16n;
+      for (int r = 0; r < 16; ++r) y[j][r] = __builtin_fmaf(s, acc[j][r], y[j][r]);
+  };
+  Codes even, odd;
+  fetch(even, 0, 0);
+  int g = 0;
+  for (; g + 1 < groups; g += 2) {
+    step(g, std::integral_constant<int, 0>(), even, odd);
+    step(g + 1, std::integral_constant<int, 1>(), odd, even);
   }
+  if (g < groups) step(g, std::integral_constant<int, 0>(), even, odd);
+  __syncthreads();
+  add_sums((groups - 1) & 1);
   if (n >= a.n_out) return;
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int row = row0 + 32 * t + 8 * (r >> 2) + 4 * hl + (r & 3);
+      const int row = row0 + 32 * (t ^ wave) + 8 * (r >> 2) + 4 * hl + (r & 3);
       if (row < a.rows) *y_at(a, row, n) = (uint16_t)pack_bf16(y[t][r], 0.f);
     }
 }

@@ -297,9 +297,11 @@ __global__ __launch_bounds__(256, 2) void linear_tile_kernel(LinearArgs a, int r
   __shared__ __attribute__((aligned(1024))) char lds_raw[kQLds];
   lds_char* const lds = (lds_char*)lds_raw;
   const int lane = lane_id(), wave = wave_id(), hl = lane >> 5, col = lane & 31, groups = a.n_in / kQGroup;
-  // neighbours on an XCD share the outputs and take the row tiles in turn
-  const int per = (gridDim.x + 7) / 8, at = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  const int row0 = at % row_tiles * kQTile, n0 = at / row_tiles * kQTile;
+  // an XCD takes consecutive numbers, of which 64 run at a time: 8 row tiles and 8 of outputs
+  const int per = (gridDim.x + 7) / 8, at = (blockIdx.x & 7) * per + (blockIdx.x >> 3), n_tiles = (a.n_out + kQTile - 1) / kQTile;
+  const int band = at / (8 * n_tiles), in = at - band * 8 * n_tiles, high = row_tiles - 8 * band < 8 ? row_tiles - 8 * band : 8;
+  if (high <= 0) return;
+  const int row0 = (8 * band + in % high) * kQTile, n0 = in / high * kQTile;
   if (n0 >= a.n_out) return;
   const int n = n0 + 32 * wave + col, nc = n < a.n_out ? n : a.n_out - 1;
   const char* const codes = a.codes + (int64_t)nc * (a.n_in / 2) + 32 * hl;
@@ -434,6 +436,23 @@ hipError_t few_turns(hipStream_t s, const LinearArgs& a) {
   return groups >= 4 * W ? few_go<RX, NT, 4, W, S>(s, a) : groups >= 2 * W ? few_go<RX, NT, 2, W, S>(s, a) : few_go<RX, NT, 1, W, S>(s, a);
 }
 
+// Rows of a workgroup: 16, 32 or 64 in the kernel for few rows, 128 in the other.  Microseconds of each, from the rounds that its
+// workgroups take (g: groups of channels; two workgroups of the first and the last fit a compute unit, one of the others), fitted to
+// hidden sizes of 1024 to 8192 and 1 to 4096 rows.  Measured there, at 4096 x 4096: 64 rows 12.1 with 64 a workgroup, 256 rows 25 and,
+// with 128, 45, 512 rows 48 and 46, 1024 rows 94 and 47; at 8192 x 8192: 256 rows 88 and 85.
+int linear_form(int64_t rows, int64_t n_out, int g) {
+  auto few = [&](int64_t r, int64_t outs) { return ceil_div(rows, r) * ceil_div(n_out, outs); };
+  const int64_t w16 = few(16, 16), w32 = few(32, 32), w64 = few(64, 32), t = few(kQTile, kQTile), rest = t % 512;
+  const double us[4] = {1.3 + (w16 <= 256 ? 0.11 * g : (double)ceil_div(w16, 512) * 0.18 * g),
+                        1.3 + (double)ceil_div(w32, 256) * (0.5 + 0.18 * g),
+                        1.5 + (double)ceil_div(w64, 256) * (1.5 + 0.30 * g),
+                        (double)(t / 512) * (3 + 2.5 * g) + (rest == 0 ? 0 : rest <= 256 ? 3 + 1.33 * g : 3 + 2.4 * g)};
+  int best = 0;
+  for (int i = 1; i < 4; ++i)
+    if (us[i] < us[best]) best = i;
+  return 16 << best;
+}
+
 }  // namespace
 
 }  // namespace hi
@@ -482,13 +501,15 @@ extern "C" hi_status hi_linear_quantized(void* stream, const void* x_dev, const 
   hipError_t e = hipSuccess;
   if (n_rows <= 4) e = few_turns<1, 1, 8, 4>(st, a);
   else if (n_rows <= 8) e = few_turns<2, 1, 8, 3>(st, a);
-  else if (n_rows <= 16) e = few_turns<4, 1, 8, 2>(st, a);
-  else if (n_rows <= 32) e = few_turns<8, 2, 8, 2>(st, a);
-  else if (n_rows <= 64) e = few_turns<16, 2, 4, 2>(st, a);
-  else {
-    const int64_t row_tiles = ceil_div(n_rows, kQTile), tiles = row_tiles * ceil_div(n_out, kQTile);
-    if (tiles > 0x7FFFFFF0) { set_last_error("quantised linear: too many rows"); return HI_ERR_RANGE; }
-    hipLaunchKernelGGL(linear_tile_kernel, dim3((unsigned)(8 * ceil_div(tiles, 8))), dim3(256), 0, st, a, (int)row_tiles);
+  else switch (linear_form(n_rows, n_out, n_in / kQGroup)) {
+    case 16: e = few_turns<4, 1, 8, 2>(st, a); break;
+    case 32: e = few_turns<8, 2, 8, 2>(st, a); break;
+    case 64: e = few_turns<16, 2, 4, 2>(st, a); break;
+    default: {
+      const int64_t row_tiles = ceil_div(n_rows, kQTile), tiles = row_tiles * ceil_div(n_out, kQTile);
+      if (tiles > 0x7FFFFFF0) { set_last_error("quantised linear: too many rows"); return HI_ERR_RANGE; }
+      hipLaunchKernelGGL(linear_tile_kernel, dim3((unsigned)(8 * ceil_div(tiles, 8))), dim3(256), 0, st, a, (int)row_tiles);
+    }
   }
   if (e != hipSuccess) { set_last_error("quantised linear: %s", hipGetErrorString(e)); return HI_ERR_HIP; }
   return launched("quantised linear");

@@ -249,12 +249,28 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
     lds_char* const kt = lds + stage * kStageBytes;
     lds_char* const vt = kt + kTileBytes;
 
-    // register r of sub-block sb: the lane's row against key 32 sb + 8 (r / 4) + 4 hl + r % 4 of the tile
+    // register r of sub-block sb: the lane's row against key 32 sb + 8 (r / 4) + 4 hl + r % 4 of the tile.  Operands are read four
+    // ahead of the products that take them: left to itself the compiler reads each where it is needed, and the products wait for LDS.
+    constexpr int A = 4;
+    bf16x8 op[A + 1];
     f32x16 s[2];
+    auto read_k = [&](int i) __attribute__((always_inline)) { op[i % (A + 1)] = *(lds_bf16x8*)(kt + lc.koff[i >> 1] + (i & 1) * 8192); };
+    auto read_v = [&](int i) __attribute__((always_inline)) {
+      lds_char* const p = vt + lc.voff[i & 3] + (i >> 2) * 4096;
+      const bf16x4 v0 = lds_read_tr8(p), v1 = lds_read_tr8(p + 2048);
+      op[i % (A + 1)] = (bf16x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
 #pragma unroll
     for (int r = 0; r < 16; ++r) { s[0][r] = 0.f; s[1][r] = 0.f; }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(lds_bf16x8*)(kt + lc.koff[i >> 1] + (i & 1) * 8192), qf[i >> 1], s[i & 1], 0, 0, 0);
+    for (int i = 0; i < A; ++i) read_k(i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (i + A < 16) read_k(i + A);
+      s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i % (A + 1)], qf[i >> 1], s[i & 1], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     lds_char* const sc = lds + kScalesAt + stage * 2 * kTileRows * 4 + 16 * hl;
     if constexpr (BITS == 8) {
 #pragma unroll
@@ -304,33 +320,36 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
     // weights, rounded to bf16 for the matrix pipe; their sum is that of the fp32 values
     u32x4 pw[2][2];
     float lq[4];
+    auto weights = [&](int sb, int u, int h) __attribute__((always_inline)) {      // four of them: registers 8 u + 4 h ..
+      float p[4];
 #pragma unroll
-    for (int sb = 0; sb < 2; ++sb)
+      for (int e = 0; e < 4; ++e) p[e] = fast_exp2(__builtin_fmaf(s[sb][8 * u + 4 * h + e], a.c, -mc));
+      float& sum = lq[2 * sb + u];
+      sum = (h == 0 ? 0.f : sum) + ((p[0] + p[1]) + (p[2] + p[3]));
+      if constexpr (BITS == 8) {
+        const f32x4 f = *(lds_f32x4*)(sc + (kTileRows + 32 * sb + 16 * u + 8 * h) * 4);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float p[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = fast_exp2(__builtin_fmaf(s[sb][8 * u + e], a.c, -mc));
-        lq[2 * sb + u] = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-        if constexpr (BITS == 8) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const f32x4 f = *(lds_f32x4*)(sc + (kTileRows + 32 * sb + 16 * u + 8 * h) * 4);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) p[4 * h + r] *= f[r];
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) pw[sb][u][e] = pack_bf16(p[2 * e], p[2 * e + 1]);
+        for (int r = 0; r < 4; ++r) p[r] *= f[r];
       }
-    st.l += (lq[0] + lq[1]) + (lq[2] + lq[3]);
+      uint32_t w0 = pack_bf16(p[0], p[1]), w1 = pack_bf16(p[2], p[3]);
+      asm volatile("" : "+v"(sum), "+v"(w0), "+v"(w1));                            // here, and not where they are next used
+      pw[sb][u][2 * h] = w0;
+      pw[sb][u][2 * h + 1] = w1;
+    };
+#pragma unroll
+    for (int i = 0; i < A; ++i) read_v(i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) weights(0, i >> 1, i & 1);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      lds_char* const p = vt + lc.voff[i & 3] + (i >> 2) * 4096;
-      const bf16x4 v0 = lds_read_tr8(p), v1 = lds_read_tr8(p + 2048);
-      st.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16((bf16x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7),
-                                                          __builtin_bit_cast(bf16x8, pw[i >> 3][(i >> 2) & 1]), st.o[i & 3], 0, 0, 0);
+      if (i + A < 16) read_v(i + A);
+      st.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i % (A + 1)], __builtin_bit_cast(bf16x8, pw[i >> 3][(i >> 2) & 1]), st.o[i & 3], 0, 0, 0);
+      if (i < 8 && (i & 1)) weights(1, i >> 2, (i >> 1) & 1);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    st.l += (lq[0] + lq[1]) + (lq[2] + lq[3]);
     if (j + 1 < n) settle(1 - stage);
   }
 

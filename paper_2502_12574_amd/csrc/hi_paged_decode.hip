@@ -426,12 +426,13 @@ __global__ __launch_bounds__(256, 1) void paged_decode_kernel(PagedAttnArgs a) {
     }
     if (!whole) {
       const int first = begin / run, last = (done - 1) / run;
-      __threadfence();
+      // Pieces are written and read by device-scope accesses that no L2 keeps a copy of, so the wait for the stores, the barrier and the
+      // count order them; a release or acquire of everything else would walk the whole L2 (1000 rows of 8 heads: 21 us instead of 8).
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
-      if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(a.arrivals + first, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+      if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(a.arrivals + first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       __syncthreads();
       if (arrived == last - first) {                               // the others' pieces are there
-        __threadfence();
         gather_pieces(a.pieces, first, last, cols, red, a.c, lane, wave);
         __syncthreads();
         for (int i = threadIdx.x; i < cols * 64; i += 256) {

@@ -4,10 +4,11 @@
 
 namespace hi {
 
-// hi_paged_decode.hip: runs of tiles, one a workgroup (one workgroup for each of the 256 compute units, whose LDS it fills), no shorter
-// than two tiles for each of its wavefronts; pieces of blocks that lie in several runs, at most two a run
+// hi_paged_decode.hip: runs of 32-row tiles, one a workgroup (one workgroup for each of the 256 compute units, whose LDS it fills), no
+// shorter than a tile for each of its wavefronts; pieces of blocks that lie in several runs, at most two a run; three arrays of counts
 constexpr int kPagedRuns = 256;
-constexpr int kPagedLeastRun = 8;
+constexpr int kPagedLeastRun = 4;
+constexpr int kPagedArrivals = 3 * kPagedRuns;
 constexpr int kPagedPieceFloats = 16 * kPartialFloats;
 
 // hi_paged_chunk.hip: two workgroups of 128 rows a compute unit; blocks that are cut leave an image of their state (64 O^T accumulators,

@@ -6,7 +6,7 @@ namespace hi {
 namespace {
 
 // The workspace: arrival counts, then either the pieces of the one kernel or the images of the other.
-constexpr int kArrivalBytes = kPagedRuns * 4;
+constexpr int kArrivalBytes = kPagedArrivals * 4;
 
 // Pieces of a block: the fewest rounds of workgroups, counted in tiles of the longest block; a workgroup costs about 6 tiles to begin
 // and to end, a merge 10.

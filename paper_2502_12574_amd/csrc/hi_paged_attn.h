@@ -8,6 +8,7 @@ namespace hi {
 // shorter than a tile for each of its wavefronts; pieces of blocks that lie in several runs, at most two a run; three arrays of counts
 constexpr int kPagedRuns = 256;
 constexpr int kPagedLeastRun = 4;
+template <int BITS> constexpr int kPagedStart = BITS == 8 ? 12 : 6;
 constexpr int kPagedArrivals = 3 * kPagedRuns;
 constexpr int kPagedPieceFloats = 16 * kPartialFloats;
 

@@ -3,7 +3,8 @@
 //
 // Work.  A block is the new rows of one sequence that fit 16 columns with the query heads of one KV head (16 / group positions);
 // it sweeps its sequence's keys in tiles of 32 rows, two halves that never cross a page.  The tiles of all blocks of all heads of all
-// sequences, one after the other, are cut into equal runs, one for each workgroup, whatever the lengths are; where there are so few
+// sequences, one after the other, are cut into equal runs, one for each workgroup, whatever the lengths are (a block counts for
+// kPagedStart tiles more: its first loads and its merge are not hidden by anything); where there are so few
 // that every block can be cut into equal pieces of at most a run without more pieces than workgroups, a workgroup takes such a piece
 // instead.  Every workgroup finds its part from the lengths themselves, so nothing is planned on the host and a captured launch
 // follows them.  A block that lies in several parts is merged by the workgroup that finishes last: by sixteens, then the sixteens.
@@ -332,25 +333,36 @@ __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
     mine = s0 + lane < S ? paged_seq_of(a.seqs, s0 + lane) : PagedSeq{0, 0, 0};
     mw = seq_work(a, mine);
   };
-  int total = 0;
+  constexpr int kStart = kPagedStart<BITS>;
+  int tiles_of_all = 0, items_of_all = 0;
   float about = 0.f;                                               // (a batch whose sequences overlap could overflow the count)
   for (int s0 = 0; s0 < S; s0 += 64) {
     look(s0);
-    total += __builtin_amdgcn_readlane(sum_wave(mw.tiles * mw.items), 63);
-    about += over_wave((float)mw.tiles * (float)mw.items, op_add);
+    tiles_of_all += __builtin_amdgcn_readlane(sum_wave(mw.tiles * mw.items), 63);
+    items_of_all += __builtin_amdgcn_readlane(sum_wave(mw.items), 63);
+    about += over_wave((float)(mw.tiles + kStart) * (float)mw.items, op_add);
   }
   if (about > 2.1e9f) return;
-  int run = (int)(((uint32_t)total + gridDim.x - 1) / gridDim.x);
-  run = run < kPagedLeastRun ? kPagedLeastRun : run;
-  int pieces = 0;                                                  // (no overflow: at most total of them)
-  for (int s0 = 0; s0 < S; s0 += 64) {
-    if (S > 64) look(s0);
-    pieces += __builtin_amdgcn_readlane(sum_wave((int)((uint32_t)(mw.tiles + run - 1) / (uint32_t)run) * mw.items), 63);
+  const uint32_t wgs = gridDim.x;
+  // equal pieces: as small as a workgroup each allows, or a quarter larger
+  uint32_t piece_tiles = ((uint32_t)tiles_of_all + wgs - 1) / wgs;
+  piece_tiles = piece_tiles < kPagedLeastRun ? kPagedLeastRun : piece_tiles;
+  int pieces = 0;
+  bool by_piece = false;
+#pragma unroll
+  for (int attempt = 0; attempt < 2 && !by_piece; ++attempt) {
+    if (attempt == 1) piece_tiles += piece_tiles / 4 + 1;
+    pieces = 0;                                                    // (at most as many as tiles)
+    for (int s0 = 0; s0 < S; s0 += 64) {
+      if (S > 64) look(s0);
+      pieces += __builtin_amdgcn_readlane(sum_wave((int)((mw.tiles + piece_tiles - 1) / piece_tiles) * mw.items), 63);
+    }
+    by_piece = pieces <= (int)wgs;
   }
-  // From here on a block has units: its tiles, or its equal pieces if a workgroup takes one of them.
-  const bool by_piece = pieces <= (int)gridDim.x;
-  auto units_of = [&](int tiles) __attribute__((always_inline)) { return by_piece ? (int)((uint32_t)(tiles + run - 1) / (uint32_t)run) : tiles; };
-  const int step = by_piece ? 1 : run, all = by_piece ? pieces : total;
+  const int total = tiles_of_all + kStart * items_of_all, run = (int)(((uint32_t)total + wgs - 1) / wgs);
+  // From here on a block has units: its start and its tiles, or its equal pieces if a workgroup takes one of them.
+  auto units_of = [&](int tiles) __attribute__((always_inline)) { return by_piece ? (int)((tiles + piece_tiles - 1) / piece_tiles) : tiles + kStart; };
+  const int step = by_piece ? 1 : run, all = by_piece ? pieces : total, start = by_piece ? 0 : kStart;
   int at = blockIdx.x * step;
   if (at >= all) return;
   const int end = at + step < all ? at + step : all;
@@ -392,8 +404,9 @@ __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
     const int begin = before + item * units, done = begin + units;       // the block's units among all
     const int b = (int)((uint32_t)item / (uint32_t)a.pool.heads), kv = item - b * a.pool.heads;
     const int u0 = at - begin, u1 = (end < done ? end : done) - begin;
-    const int t0 = by_piece ? (int)((uint64_t)w.tiles * (uint32_t)u0 / (uint32_t)units) : u0;
-    const int t1 = by_piece ? (int)((uint64_t)w.tiles * (uint32_t)u1 / (uint32_t)units) : u1;
+    if (u1 <= start) return;                                       // (a run that ends in a block's start: the next one begins it)
+    const int t0 = by_piece ? (int)((uint64_t)w.tiles * (uint32_t)u0 / (uint32_t)units) : u0 > start ? u0 - start : 0;
+    const int t1 = by_piece ? (int)((uint64_t)w.tiles * (uint32_t)u1 / (uint32_t)units) : u1 - start;
 
     const int row0 = sq.first + b * a.positions;
     const int rows = sq.rows - b * a.positions < a.positions ? sq.rows - b * a.positions : a.positions;
@@ -525,10 +538,10 @@ __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
       __syncthreads();
       return arrived == want;
     };
-    if (u0 == 0 && u1 == units) {
+    if (t0 == 0 && t1 == w.tiles) {
       put(nullptr);
     } else {
-      const int first = begin / step, last = (done - 1) / step, me = blockIdx.x;
+      const int first = (begin + start) / step, last = (done - 1) / step, me = blockIdx.x;
       auto piece_of = [&](int p) __attribute__((always_inline)) { return a.pieces + (int64_t)(2 * p + (p == first)) * kPiece; };
       const int fan = (me - first) / kFan, lead = first + fan * kFan, n_fan = last - lead + 1 < kFan ? last - lead + 1 : kFan, fans = (last - first) / kFan + 1;
       put(piece_of(me));

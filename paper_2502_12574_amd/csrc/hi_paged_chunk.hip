@@ -159,8 +159,9 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
     return __builtin_amdgcn_readlane(pages, j & 63);
   };
 
-  u32x4 kreg[2], vreg[2];                        // 8-bit rows on their way
-  float screg = 0.f;
+  u32x4 k_lo = {0, 0, 0, 0}, k_hi = k_lo, v_lo = k_lo, v_hi = k_lo;      // 8-bit rows on their way
+  float row_scale = 0.f;
+  bool staged = false;
   const uint32_t lds_wave = (uint32_t)(uintptr_t)lds + wave * 4096;
   auto fetch = [&](int j, int stage) __attribute__((always_inline)) {
     const int page = page_of(j), row = group_row(j), last = w.len - 1 - row;     // rows past the end re-read the last one
@@ -177,35 +178,40 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
         g2lds16_s<0>(v, (uint32_t)(from * kRowBytes + ((p ^ swz_v(r)) << 4)), to + kTileBytes + i * 1024);
       }
     } else {
+      // (of a page that is not there: the first page's, which count for nothing and are made zeros on their way to LDS)
       const char* const k = a.pool.pages + at * kHeadDim;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int r = 8 * i + (lane >> 3), from = r < last ? r : last;
-        kreg[i] = vreg[i] = (u32x4){0, 0, 0, 0};
-        if (ok) {
-          kreg[i] = *(const u32x4*)(k + from * kHeadDim + 16 * (lane & 7));
-          vreg[i] = *(const u32x4*)(k + (((int64_t)kHeadDim) << a.pool.shift) + from * kHeadDim + 16 * (lane & 7));
-        }
-      }
-      const int r = lane & 15;
-      screg = ok && lane < 32 ? a.pool.scales[at + (r < last ? r : last) + (lane < 16 ? 0 : in_page + 1)] : 0.f;
+      const char* const v = k + ((int64_t)kHeadDim << a.pool.shift);
+      const int r0 = lane >> 3, r1 = r0 + 8, clip = ok ? last : 15, r = lane & 15;
+      const uint32_t at0 = (r0 < clip ? r0 : clip) * kHeadDim + 16 * (lane & 7), at1 = (r1 < clip ? r1 : clip) * kHeadDim + 16 * (lane & 7);
+      k_lo = *(const u32x4*)(k + at0);
+      k_hi = *(const u32x4*)(k + at1);
+      v_lo = *(const u32x4*)(v + at0);
+      v_hi = *(const u32x4*)(v + at1);
+      row_scale = a.pool.scales[at + (r < clip ? r : clip) + (lane & 16 ? in_page + 1 : 0)];
+      staged = ok;
     }
   };
   auto settle = [&](int stage) __attribute__((always_inline)) {        // 8-bit rows into LDS, as bf16
     if constexpr (BITS == 8) {
       lds_char* const to = lds + stage * kStageBytes + wave * 4096;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int r = 8 * i + (lane >> 3), p = lane & 7;
-        u32x4 lo, hi;
-        widen(kreg[i], lo, hi);
-        *(lds_u32x4*)(to + r * kRowBytes + (((2 * p) ^ swz_k(r)) << 4)) = lo;
-        *(lds_u32x4*)(to + r * kRowBytes + (((2 * p + 1) ^ swz_k(r)) << 4)) = hi;
-        widen(vreg[i], lo, hi);
-        *(lds_u32x4*)(to + kTileBytes + r * kRowBytes + (((2 * p) ^ swz_v(r)) << 4)) = lo;
-        *(lds_u32x4*)(to + kTileBytes + r * kRowBytes + (((2 * p + 1) ^ swz_v(r)) << 4)) = hi;
+      const int r0 = lane >> 3, p = lane & 7;
+      const uint32_t ka = r0 * kRowBytes + (((2 * p) ^ swz_k(r0)) << 4), va = kTileBytes + r0 * kRowBytes + (((2 * p) ^ swz_v(r0)) << 4);
+      if (!staged) {
+        k_lo = k_hi = v_lo = v_hi = (u32x4){0, 0, 0, 0};
+        row_scale = 0.f;
       }
-      if (lane < 32) *(lds_float*)(lds + kScalesAt + ((stage * 2 + (lane >> 4)) * kTileRows + 16 * wave + (lane & 15)) * 4) = screg;
+      // (8 rows on, the swizzle of a K row changes by 8, that of a V row not at all; the second chunk's lies 1 apart)
+      auto put = [&](uint32_t off, const u32x4& b) __attribute__((always_inline)) {
+        u32x4 lo, hi;
+        widen(b, lo, hi);
+        *(lds_u32x4*)(to + off) = lo;
+        *(lds_u32x4*)(to + (off ^ 16)) = hi;
+      };
+      put(ka, k_lo);
+      put((ka ^ 128) + 8 * kRowBytes, k_hi);
+      put(va, v_lo);
+      put(va + 8 * kRowBytes, v_hi);
+      if (lane < 32) *(lds_float*)(lds + kScalesAt + ((stage * 2 + (lane >> 4)) * kTileRows + 16 * wave + (lane & 15)) * 4) = row_scale;
     }
   };
   fetch(0, 0);
@@ -229,6 +235,7 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
     }
   }
   const int lim = w.sees + mine.pos < w.len ? w.sees + mine.pos : w.len - 1;     // the last key the lane's row sees
+  const bool works = 32 * wave < w.rows * a.group;
   const Lane lc = lane_offsets(lane);
   State st;
   st.m = kNegBig;
@@ -248,6 +255,10 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
     if (j + 1 < n) fetch(j + 1, 1 - stage);
     lds_char* const kt = lds + stage * kStageBytes;
     lds_char* const vt = kt + kTileBytes;
+    if (!works) {                                // (no row of the wavefront's is a row of the block)
+      if (j + 1 < n) settle(1 - stage);
+      continue;
+    }
 
     // register r of sub-block sb: the lane's row against key 32 sb + 8 (r / 4) + 4 hl + r % 4 of the tile.  Operands are read four
     // ahead of the products that take them: left to itself the compiler reads each where it is needed, and the products wait for LDS.
@@ -353,6 +364,7 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
     if (j + 1 < n) settle(1 - stage);
   }
 
+  if (!works) return;
   const float l = both_halves(st.l, false);
   if (a.split == 1) {
     const float inv = l > 0.f ? 1.0f / l : 0.f;
@@ -375,7 +387,7 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   const int lane = lane_id(), wave = wave_id(), unit = blockIdx.x, db = blockIdx.y;
   const ChunkWork w = chunk_work(a, unit, 0, lane);
-  if (!w.any) return;
+  if (!w.any || 32 * wave >= w.rows * a.group) return;
   const LaneRow mine = lane_row(a, w, 32 * wave + (lane & 31));
   const float* const images = a.images + (int64_t)unit * a.split * kPagedImageFloats + threadIdx.x;
   float m = kNegBig, l = 0.f;

@@ -12,10 +12,11 @@ template <int BITS> constexpr int kPagedStart = BITS == 8 ? 12 : 6;
 constexpr int kPagedArrivals = 3 * kPagedRuns;
 constexpr int kPagedPieceFloats = 16 * kPartialFloats;
 
-// hi_paged_chunk.hip: two workgroups of 128 rows a compute unit; blocks that are cut leave an image of their state (64 O^T accumulators,
-// m and l for each of 256 lanes) for each piece, in at most kPagedMostPieces of them
+// hi_paged_chunk.hip: two workgroups of 128 rows a compute unit; a block that is cut leaves an image of its state (64 O^T accumulators, m
+// and l for each of 256 lanes) for each piece.  Pieces have at least the tiles of all blocks / (2 x 512), so there are at most twice
+// as many images as that.
 constexpr int kPagedSlots = 512;
-constexpr int kPagedMostPieces = 1024;
+constexpr int kPagedMostImages = 4 * kPagedSlots;
 constexpr int kPagedImageFloats = 66 * 256;
 
 struct PagedAttnArgs {
@@ -24,7 +25,6 @@ struct PagedAttnArgs {
   int q_heads, group;
   int positions, by_group;       // positions of a block; 65536 / group, rounded up
   float c;                       // what a score is multiplied by before the power of two
-  int split;                     // pieces of a block's tiles, each a workgroup's
   int* arrivals; float* pieces; float* images;   // in the workspace
 };
 

@@ -8,18 +8,6 @@ namespace {
 // The workspace: arrival counts, then either the pieces of the one kernel or the images of the other.
 constexpr int kArrivalBytes = kPagedArrivals * 4;
 
-// Pieces of a block: the fewest rounds of workgroups, counted in tiles of the longest block; a workgroup costs about 6 tiles to begin
-// and to end, a merge 10.
-int chunk_split(int64_t units, int64_t tiles) {
-  int best = 1;
-  double least = 1e300;
-  for (int k = 1; k <= 64 && (k == 1 || units * k <= kPagedMostPieces); ++k) {
-    const double t = (double)ceil_div(units * k, kPagedSlots) * ((double)tiles / k + 6) + (k > 1 ? 10 : 0);
-    if (t < least) { least = t; best = k; }
-  }
-  return best;
-}
-
 }  // namespace
 
 }  // namespace hi
@@ -29,7 +17,7 @@ using namespace hi;
 extern "C" hi_status hi_paged_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int64_t* bytes) {
   if (!bytes || n_kv_heads < 1 || n_q_heads < 1 || n_q_heads % n_kv_heads != 0) { set_last_error("paged workspace: bad argument"); return HI_ERR_ARG; }
   if (n_q_heads / n_kv_heads > 16) { set_last_error("paged attention: at most 16 query heads a KV head"); return HI_ERR_UNSUPPORTED; }
-  const int64_t pieces = (int64_t)2 * kPagedRuns * kPagedPieceFloats * 4, images = (int64_t)kPagedMostPieces * kPagedImageFloats * 4;
+  const int64_t pieces = (int64_t)2 * kPagedRuns * kPagedPieceFloats * 4, images = (int64_t)kPagedMostImages * kPagedImageFloats * 4;
   *bytes = kArrivalBytes + (pieces > images ? pieces : images);
   return HI_OK;
 }
@@ -69,6 +57,5 @@ extern "C" hi_status hi_paged_attn(void* stream, const hi_paged_cache* cache, co
   // blocks of all sequences: each but the last of a sequence is full, and each has a row
   const int64_t blocks = batch->n_rows / a.positions + batch->n_seqs;
   const int64_t units = (blocks < batch->n_rows ? blocks : batch->n_rows) * cache->n_kv_heads;
-  a.split = chunk_split(units, ceil_div(table_rows, 64));
   return launch_paged_chunk(stream, a, units);
 }

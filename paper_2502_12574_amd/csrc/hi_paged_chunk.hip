@@ -1,10 +1,11 @@
 // Attention of a chunk of new rows of each of many sequences over a pool of cache pages: the matrix rate is the bound.
 //
 // Work.  A block is 128 rows of one sequence and one KV head: 128 / group consecutive positions with the query heads of that KV head,
-// so that its rows share the keys.  It sweeps its sequence's keys in tiles of 64; a workgroup takes a block, or one of `split` equal
-// pieces of its tiles where the blocks alone would not fill the chip (merged by paged_merge_kernel).  KV heads change fastest in the
-// numbering, deep blocks come first: with 8 heads each XCD sweeps one of them, and the workgroups that sweep the same tiles at the
-// same time find them in its L2.
+// so that its rows share the keys.  It sweeps its sequence's keys in tiles of 64; a workgroup takes a block, or, where long blocks alone
+// would not fill the chip, one of the equal pieces into which all blocks of the sequence are cut (merged by paged_merge_kernel).  Every
+// workgroup works the cut out from the lengths themselves, so a captured launch follows them.  KV heads change fastest in the
+// numbering, then blocks, deep ones first: with 8 heads each XCD sweeps one of them, and the workgroups that sweep the same tiles at
+// the same time find them in its L2.  (Runs of equal numbers of tiles, as for few rows, would lose that.)
 //
 // A wavefront holds 32 rows.  S^T = K Q^T (32x32x16 tiles) leaves a row in one lane column: its running maximum and sum are per lane,
 // and the weights, rounded to bf16, are the B operand of O^T += V^T P^T as they lie.  bf16 tiles go to LDS by direct loads; rows of
@@ -72,46 +73,106 @@ __device__ __forceinline__ void widen(u32x4 b, u32x4& lo, u32x4& hi) {
   }
 }
 
-// What a workgroup does: its block, and the tiles [t0, t1) of it.
-struct ChunkWork { int seq, kv, row0, rows, tiles, t0, t1, sees, len; bool any; };
-__device__ __forceinline__ ChunkWork chunk_work(const PagedAttnArgs& a, int unit, int piece, int lane) {
+// A sequence's share: tiles of its deepest block, blocks of a head.
+struct SeqBlocks { int tiles, blocks; };
+__device__ __forceinline__ SeqBlocks seq_blocks(const PagedAttnArgs& a, const PagedSeq& q) {
+  const int64_t len = (int64_t)q.past + q.rows, most = (int64_t)a.seqs.table_pages << a.pool.shift;
+  return {(int)(((len < most ? len : most) + kTileRows - 1) / kTileRows), (int)((uint32_t)(q.rows + a.positions - 1) / (uint32_t)a.positions)};
+}
+__device__ __forceinline__ int pieces_of(int tiles, uint32_t piece) { return (int)((tiles + piece - 1) / piece); }
+
+// What a workgroup does: its block, and the tiles [t0, t1) of it; pieces of the block, the block's first image and the distance of the
+// next piece's (number: the workgroup's, or with MERGE the block's).
+struct ChunkWork { int seq, kv, row0, rows, tiles, t0, t1, sees, len, pieces, piece, image, next_image; bool any; };
+template <bool MERGE>
+__device__ __forceinline__ ChunkWork chunk_work(const PagedAttnArgs& a, int number, int lane) {
   ChunkWork w;
   w.any = false;
-  w.kv = unit % a.pool.heads;
-  const int nth = unit / a.pool.heads;
-  int before = 0;
-  for (int s0 = 0; s0 < a.seqs.n_seqs; s0 += 64) {
-    int mine = 0;
-    if (s0 + lane < a.seqs.n_seqs) mine = (paged_seq_of(a.seqs, s0 + lane).rows + a.positions - 1) / a.positions;
-    int upto = mine;
+  const int S = a.seqs.n_seqs, H = a.pool.heads;
+  PagedSeq q = {0, 0, 0};
+  SeqBlocks sb = {0, 0};
+  auto look = [&](int s0) __attribute__((always_inline)) {
+    q = s0 + lane < S ? paged_seq_of(a.seqs, s0 + lane) : PagedSeq{0, 0, 0};
+    sb = seq_blocks(a, q);
+  };
+  uint32_t total = 0;
+  int longest = 1;
+  float about = 0.f;                             // (a batch whose sequences overlap could overflow the count)
+  for (int s0 = 0; s0 < S; s0 += 64) {
+    look(s0);
+    total += __builtin_amdgcn_readlane(sum_wave(sb.tiles * sb.blocks * H), 63);
+    about += over_wave((float)sb.tiles * (float)sb.blocks * (float)H, op_add);
+    const int most = (int)over_wave((float)(sb.blocks > 0 ? sb.tiles : 0), op_max);      // (as near as is needed)
+    longest = most > longest ? most : longest;
+  }
+  if (about > 2.1e9f) return w;
+  // Whole blocks, or pieces of the tiles of all blocks over one or two rounds: a workgroup costs 6 tiles to begin and to end, a merge 3
+  // and one for every 70 images, and a round ends with its longest piece unless the short ones that follow fill its gaps.
+  uint32_t piece = longest;
+  float least = 0.f;
 #pragma unroll
-    for (int off = 1; off < 64; off *= 2) {
-      const int y = __shfl_up(upto, off);
-      if (lane >= off) upto += y;
+  for (int i = 0; i < 3; ++i) {
+    uint32_t size = i == 0 ? (uint32_t)longest : (total + i * kPagedSlots - 1) / (i * kPagedSlots);
+    size = size < 4 ? 4 : size;
+    if (i > 0 && size >= (uint32_t)longest) break;
+    int n = 0;
+    for (int s0 = 0; s0 < S; s0 += 64) {
+      if (S > 64) look(s0);
+      n += __builtin_amdgcn_readlane(sum_wave(pieces_of(sb.tiles, size) * sb.blocks * H), 63);
     }
-    const int n = __popcll(__builtin_amdgcn_ballot_w64(before + upto <= nth));
+    const float rounds = (float)((n + kPagedSlots - 1) / kPagedSlots) * ((float)size + 6.f);
+    const float filled = ((float)total + 6.f * (float)n) * (1.f / kPagedSlots) + (float)size;
+    const float cost = fminf(rounds, filled) + (i == 0 ? 0.f : 3.f + (float)n * (1.f / 70.f));
+    if (i == 0 || cost < least) {
+      least = cost;
+      piece = size;
+    }
+  }
+  piece = __builtin_amdgcn_readfirstlane(piece);
+  // the sequence that has the number; images: those of the sequences before it
+  int before = 0, images = 0, seq = 0, n_blocks = 0, k = 1;
+  for (int s0 = 0; s0 < S; s0 += 64) {
+    if (S > 64) look(s0);
+    const int cut = pieces_of(sb.tiles, piece), here = sb.blocks * H * (MERGE ? 1 : cut), kept = cut > 1 ? sb.blocks * H * cut : 0;
+    const int upto = sum_wave(here), images_upto = sum_wave(kept);
+    const int n = __popcll(__builtin_amdgcn_ballot_w64(before + upto <= number));
     if (n < 64) {
-      w.seq = __builtin_amdgcn_readfirstlane(s0 + n);
-      if (w.seq >= a.seqs.n_seqs) return w;
-      if (n > 0) before += __builtin_amdgcn_readlane(upto, n - 1);
+      seq = s0 + n;
+      if (n > 0) {
+        before += __builtin_amdgcn_readlane(upto, n - 1);
+        images += __builtin_amdgcn_readlane(images_upto, n - 1);
+      }
+      w.kv = __builtin_amdgcn_readlane(q.first, n);              // (for now)
+      w.rows = __builtin_amdgcn_readlane(q.rows, n);
+      w.sees = __builtin_amdgcn_readlane(q.past, n);
+      w.tiles = __builtin_amdgcn_readlane(sb.tiles, n);
+      n_blocks = __builtin_amdgcn_readlane(sb.blocks, n);
+      k = __builtin_amdgcn_readlane(cut, n);
       break;
     }
     before += __builtin_amdgcn_readlane(upto, 63);
-    w.seq = s0 + 64;
+    images += __builtin_amdgcn_readlane(images_upto, 63);
+    seq = S;
   }
-  if (w.seq >= a.seqs.n_seqs) return w;
-  const PagedSeq q = paged_seq_of(a.seqs, w.seq);
-  const int blocks = (q.rows + a.positions - 1) / a.positions, b = blocks - 1 - (nth - before);     // the deepest first
-  if (b < 0 || b >= blocks) return w;
-  w.row0 = q.first + b * a.positions;
-  w.rows = q.rows - b * a.positions < a.positions ? q.rows - b * a.positions : a.positions;
-  const int64_t most = (int64_t)a.seqs.table_pages << a.pool.shift, all = (int64_t)q.past + q.rows;
+  if (seq >= S) return w;
+  const int first = w.kv, rows = w.rows, past = w.sees;
+  const uint32_t in = number - before, of_all = in / (uint32_t)H;
+  w.seq = seq;
+  w.kv = (int)(in - of_all * H);
+  w.piece = (int)(of_all / (uint32_t)n_blocks);
+  const int nth = (int)of_all - w.piece * n_blocks, b = n_blocks - 1 - nth;      // the deepest first
+  w.pieces = k;
+  w.next_image = n_blocks * H;
+  w.image = images + nth * H + w.kv;
+  w.row0 = first + b * a.positions;
+  w.rows = rows - b * a.positions < a.positions ? rows - b * a.positions : a.positions;
+  const int64_t most = (int64_t)a.seqs.table_pages << a.pool.shift, all = (int64_t)past + rows;
   w.len = (int)(all < most ? all : most);
-  const int64_t sees = (int64_t)q.past + b * a.positions, deepest = sees + w.rows;
-  w.sees = (int)(sees < w.len ? sees : w.len - 1);                     // the last key of the block's first position
+  const int64_t sees = (int64_t)past + b * a.positions, deepest = sees + w.rows;
+  w.sees = (int)(sees < w.len ? sees : w.len - 1);                               // the last key of the block's first position
   w.tiles = (int)(((deepest < w.len ? deepest : w.len) + kTileRows - 1) / kTileRows);
-  w.t0 = (int)((int64_t)w.tiles * piece / a.split);
-  w.t1 = (int)((int64_t)w.tiles * (piece + 1) / a.split);
+  w.t0 = (int)((uint64_t)w.tiles * (uint32_t)w.piece / (uint32_t)k);
+  w.t1 = (int)((uint64_t)w.tiles * (uint32_t)(w.piece + 1) / (uint32_t)k);
   w.any = true;
   return w;
 }
@@ -138,9 +199,7 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds_raw[kLds<BITS>];
   lds_char* const lds = (lds_char*)lds_raw;
   const int lane = lane_id(), wave = wave_id(), hl = lane >> 5, col = lane & 31;
-  const int unit = blockIdx.x % a.pool.heads + blockIdx.x / (a.pool.heads * a.split) * a.pool.heads;
-  const int piece = blockIdx.x / a.pool.heads % a.split;
-  const ChunkWork w = chunk_work(a, unit, piece, lane);
+  const ChunkWork w = chunk_work<false>(a, blockIdx.x, lane);
   if (!w.any || w.t0 >= w.t1) return;
   const int n = w.t1 - w.t0;
   const int* const table = a.seqs.table + (int64_t)w.seq * a.seqs.table_pages;
@@ -366,7 +425,7 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
 
   if (!works) return;
   const float l = both_halves(st.l, false);
-  if (a.split == 1) {
+  if (w.pieces == 1) {
     const float inv = l > 0.f ? 1.0f / l : 0.f;
     if (mine.live) {
 #pragma unroll
@@ -374,7 +433,7 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
     }
     return;
   }
-  float* const image = a.images + (int64_t)(unit * a.split + piece) * kPagedImageFloats + threadIdx.x;
+  float* const image = a.images + (int64_t)(w.image + w.piece * w.next_image) * kPagedImageFloats + threadIdx.x;
 #pragma unroll
   for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -385,36 +444,63 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
 
 // Joins the pieces of a block: a workgroup for each 32 dims of it, in the lanes of the kernel above.
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
-  const int lane = lane_id(), wave = wave_id(), unit = blockIdx.x, db = blockIdx.y;
-  const ChunkWork w = chunk_work(a, unit, 0, lane);
-  if (!w.any || 32 * wave >= w.rows * a.group) return;
+  const int lane = lane_id(), wave = wave_id(), db = blockIdx.y;
+  const ChunkWork w = chunk_work<true>(a, blockIdx.x, lane);
+  if (!w.any || w.pieces == 1 || 32 * wave >= w.rows * a.group) return;
   const LaneRow mine = lane_row(a, w, 32 * wave + (lane & 31));
-  const float* const images = a.images + (int64_t)unit * a.split * kPagedImageFloats + threadIdx.x;
+  const float* const images = a.images + (int64_t)w.image * kPagedImageFloats + threadIdx.x;
+  const int64_t next = (int64_t)w.next_image * kPagedImageFloats;
+  // (a block with fewer tiles than pieces has left no image for some of them)
+  auto left = [&](int p) __attribute__((always_inline)) {
+    return (uint64_t)w.tiles * (uint32_t)p / (uint32_t)w.pieces < (uint64_t)w.tiles * (uint32_t)(p + 1) / (uint32_t)w.pieces;
+  };
   float m = kNegBig, l = 0.f;
-  for (int p = 0; p < a.split; ++p)
-    if ((int64_t)w.tiles * p / a.split < (int64_t)w.tiles * (p + 1) / a.split) m = fmaxf(m, images[(int64_t)p * kPagedImageFloats + 64 * 256]);
   f32x16 o;
 #pragma unroll
   for (int r = 0; r < 16; ++r) o[r] = 0.f;
-  for (int p = 0; p < a.split; ++p) {
-    if ((int64_t)w.tiles * p / a.split >= (int64_t)w.tiles * (p + 1) / a.split) continue;
-    const float* const x = images + (int64_t)p * kPagedImageFloats;
-    const float f = fast_exp2((x[64 * 256] - m) * a.c);
-    l += f * x[65 * 256];
+  constexpr int N = 4;                           // pieces whose loads are under way together
+  for (int p0 = 0; p0 < w.pieces; p0 += N) {
+    float pm[N], pl[N];
+    f32x16 po[N];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) o[r] += f * x[(db * 16 + r) * 256];
+    for (int i = 0; i < N; ++i) {
+      pm[i] = kNegBig;
+      pl[i] = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) po[i][r] = 0.f;
+      if (p0 + i < w.pieces && left(p0 + i)) {
+        const float* const x = images + (p0 + i) * next;
+        pm[i] = x[64 * 256];
+        pl[i] = x[65 * 256];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) po[i][r] = x[(db * 16 + r) * 256];
+      }
+    }
+    const float mn = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), m), f = fast_exp2((m - mn) * a.c);
+    m = mn;
+    l *= f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[r] *= f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float e = fast_exp2((pm[i] - m) * a.c);
+      l += e * pl[i];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[r] += e * po[i][r];
+    }
   }
   if (mine.live) write_row(a, w, mine, db, lane >> 5, o, l > 0.f ? 1.0f / l : 0.f);
 }
 
 }  // namespace
 
+// units: at least as many as there are blocks; their pieces are at most 2 x 512 more
 hi_status launch_paged_chunk(void* stream, const PagedAttnArgs& a, int64_t units) {
-  const dim3 grid((unsigned)(units * a.split));
+  const dim3 grid((unsigned)(units + 2 * kPagedSlots));
   if (a.pool.bits == 16) hipLaunchKernelGGL(paged_chunk_kernel<16>, grid, dim3(256), 0, (hipStream_t)stream, a);
   else hipLaunchKernelGGL(paged_chunk_kernel<8>, grid, dim3(256), 0, (hipStream_t)stream, a);
   const hi_status st = launched("paged attention");
-  if (st != HI_OK || a.split == 1) return st;
+  if (st != HI_OK) return st;
   hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned)units, 4), dim3(256), 0, (hipStream_t)stream, a);
   return launched("paged attention merge");
 }

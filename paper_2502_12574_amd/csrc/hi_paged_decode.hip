@@ -229,15 +229,6 @@ __device__ __forceinline__ void attend_tile(lds_char* const (&at)[2], int lane, 
   for (int db = 0; db < 8; ++db) st.o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop[db], __builtin_bit_cast(bf16x8, pw), st.o[db], 0, 0, 0);
 }
 
-// Sums over a wavefront inside the register file: of all lanes, and of the lanes up to this one.
-__device__ __forceinline__ int sum_wave(int x) {
-#define HI_DPP(ctrl, mask) x += __builtin_amdgcn_update_dpp(0, x, ctrl, mask, 0xf, false)
-  HI_DPP(0x111, 0xf); HI_DPP(0x112, 0xf); HI_DPP(0x114, 0xf); HI_DPP(0x118, 0xf);      // 1, 2, 4, 8 lanes up within 16
-  HI_DPP(0x142, 0xa); HI_DPP(0x143, 0xc);                                              // the sum of the 16, then of the 32 before
-#undef HI_DPP
-  return x;
-}
-
 // A sequence's share of the tiles.
 struct SeqWork { int tiles, items; };           // tiles of a block (the deepest one's); blocks of all heads
 __device__ __forceinline__ SeqWork seq_work(const PagedAttnArgs& a, const PagedSeq& q) {

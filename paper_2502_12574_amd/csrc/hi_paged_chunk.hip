@@ -22,6 +22,7 @@ constexpr int kTileRows = 64;
 constexpr int kTileBytes = kTileRows * kRowBytes;   // 16 KiB of K (or V), bf16
 constexpr int kStageBytes = 2 * kTileBytes;
 constexpr int kScalesAt = 2 * kStageBytes;       // [stage][K|V][64] fp32
+constexpr float kSumLimit = 4096.f;
 template <int BITS> constexpr int kLds = kScalesAt + (BITS == 8 ? 2 * 2 * kTileRows * 4 : 0);
 
 typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
@@ -222,6 +223,11 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
   float row_scale = 0.f;
   bool staged = false;
   const uint32_t lds_wave = (uint32_t)(uintptr_t)lds + wave * 4096;
+  // bf16 rows: load i brings rows 4 i .. 4 i + 3 of the 16, its offset's i KiB as an immediate (which moves the place in LDS along)
+  uint32_t k_off[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) k_off[i] = (uint32_t)((lane >> 4) * kRowBytes + (((lane & 15) ^ swz_k(4 * i + (lane >> 4))) << 4));
+  const uint32_t v_off = (uint32_t)((lane >> 4) * kRowBytes + (((lane & 15) ^ swz_v(lane >> 4)) << 4));
   auto fetch = [&](int j, int stage) __attribute__((always_inline)) {
     const int page = page_of(j), row = group_row(j), last = w.len - 1 - row;     // rows past the end re-read the last one
     const bool ok = there(page);
@@ -230,11 +236,22 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
       const char* const k = ok ? a.pool.pages + at * kRowBytes : (const char*)zero_rows;
       const char* const v = ok ? k + ((int64_t)kRowBytes << a.pool.shift) : (const char*)zero_rows;
       const uint32_t to = lds_wave + stage * kStageBytes;
+      if (!ok || last >= 15) {
+        g2lds16_s<0>(k, k_off[0], to);
+        g2lds16_s<1024>(k, k_off[1], to);
+        g2lds16_s<2048>(k, k_off[2], to);
+        g2lds16_s<3072>(k, k_off[3], to);
+        g2lds16_s<0>(v, v_off, to + kTileBytes);
+        g2lds16_s<1024>(v, v_off, to + kTileBytes);
+        g2lds16_s<2048>(v, v_off, to + kTileBytes);
+        g2lds16_s<3072>(v, v_off, to + kTileBytes);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = 4 * i + (lane >> 4), p = lane & 15, from = r < last || last < 0 ? r : last;
-        g2lds16_s<0>(k, (uint32_t)(from * kRowBytes + ((p ^ swz_k(r)) << 4)), to + i * 1024);
-        g2lds16_s<0>(v, (uint32_t)(from * kRowBytes + ((p ^ swz_v(r)) << 4)), to + kTileBytes + i * 1024);
+        for (int i = 0; i < 4; ++i) {
+          const int r = 4 * i + (lane >> 4), p = lane & 15, from = r < last ? r : last;
+          g2lds16_s<0>(k, (uint32_t)(from * kRowBytes + ((p ^ swz_k(r)) << 4)), to + i * 1024);
+          g2lds16_s<0>(v, (uint32_t)(from * kRowBytes + ((p ^ swz_v(r)) << 4)), to + kTileBytes + i * 1024);
+        }
       }
     } else {
       // (of a page that is not there: the first page's, which count for nothing and are made zeros on their way to LDS)
@@ -371,55 +388,67 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
           s[sb][r] = __uint_as_float((__float_as_uint(s[sb][r]) & t) | (__float_as_uint(kNegBig) & ~t));
         }
     }
-    float mx = s[0][0];
+    // The weights, rounded to bf16 for the matrix pipe; their sum is that of the fp32 values.  They are relative to a reference that
+    // follows the row's maximum only when it must: the lane's sum bounds each of them, and while it stays below the limit they are as
+    // harmless in fp32 and bf16 as weights up to 1.  Otherwise, and where a row has seen nothing yet, the maximum is taken.
+    u32x4 pw[2][2];
+    auto weights = [&](float mc) __attribute__((always_inline)) {
+      float lq[4];
 #pragma unroll
-    for (int sb = 0; sb < 2; ++sb)
+      for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[sb][r]);
-    const float m_new = fmaxf(st.m, both_halves(mx, true));
-    if (__builtin_amdgcn_ballot_w64(m_new > st.m) != 0) {
-      const float alpha = fast_exp2((st.m - m_new) * a.c);
+        for (int u = 0; u < 2; ++u) {
+          float p[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[e] = fast_exp2(__builtin_fmaf(s[sb][8 * u + e], a.c, -mc));
+          lq[2 * sb + u] = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+          if constexpr (BITS == 8) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const f32x4 f = *(lds_f32x4*)(sc + (kTileRows + 32 * sb + 16 * u + 8 * h) * 4);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) p[4 * h + r] *= f[r];
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) pw[sb][u][e] = pack_bf16(p[2 * e], p[2 * e + 1]);
+          if (BITS == 8) __builtin_amdgcn_sched_barrier(0);      // (or all scales would be read at once, into registers that are not there)
+        }
+      return (lq[0] + lq[1]) + (lq[2] + lq[3]);
+    };
+    if constexpr (BITS == 16) {
+#pragma unroll
+      for (int i = 0; i < A; ++i) read_v(i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    float sum = weights(st.m > kNegBig ? st.m * a.c : 0.f);
+    if (__builtin_amdgcn_ballot_w64(!(sum <= kSumLimit) || st.m == kNegBig) != 0) {       // also true for NaN
+      float mx = s[0][0];
+#pragma unroll
+      for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[sb][r]);
+      const float m_new = fmaxf(st.m, both_halves(mx, true)), alpha = fast_exp2((st.m - m_new) * a.c);
       st.l *= alpha;
 #pragma unroll
       for (int db = 0; db < 4; ++db)
 #pragma unroll
         for (int r = 0; r < 16; ++r) st.o[db][r] *= alpha;
       st.m = m_new;
+      sum = weights(st.m > kNegBig ? st.m * a.c : 0.f);            // (a row that has seen nothing yet adds weights of zero)
     }
-    const float mc = st.m > kNegBig ? st.m * a.c : 0.f;           // a row that has seen nothing yet adds weights of zero
-    // weights, rounded to bf16 for the matrix pipe; their sum is that of the fp32 values
-    u32x4 pw[2][2];
-    float lq[4];
-    auto weights = [&](int sb, int u, int h) __attribute__((always_inline)) {      // four of them: registers 8 u + 4 h ..
-      float p[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) p[e] = fast_exp2(__builtin_fmaf(s[sb][8 * u + 4 * h + e], a.c, -mc));
-      float& sum = lq[2 * sb + u];
-      sum = (h == 0 ? 0.f : sum) + ((p[0] + p[1]) + (p[2] + p[3]));
-      if constexpr (BITS == 8) {
-        const f32x4 f = *(lds_f32x4*)(sc + (kTileRows + 32 * sb + 16 * u + 8 * h) * 4);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) p[r] *= f[r];
-      }
-      uint32_t w0 = pack_bf16(p[0], p[1]), w1 = pack_bf16(p[2], p[3]);
-      asm volatile("" : "+v"(sum), "+v"(w0), "+v"(w1));                            // here, and not where they are next used
-      pw[sb][u][2 * h] = w0;
-      pw[sb][u][2 * h + 1] = w1;
-    };
-#pragma unroll
-    for (int i = 0; i < A; ++i) read_v(i);
+    st.l += sum;
     __builtin_amdgcn_sched_barrier(0);
+    if constexpr (BITS == 8) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) weights(0, i >> 1, i & 1);
-    __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < A; ++i) read_v(i);
+    }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       if (i + A < 16) read_v(i + A);
       st.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i % (A + 1)], __builtin_bit_cast(bf16x8, pw[i >> 3][(i >> 2) & 1]), st.o[i & 3], 0, 0, 0);
-      if (i < 8 && (i & 1)) weights(1, i >> 2, (i >> 1) & 1);
       __builtin_amdgcn_sched_barrier(0);
     }
-    st.l += (lq[0] + lq[1]) + (lq[2] + lq[3]);
     if (j + 1 < n) settle(1 - stage);
   }
 

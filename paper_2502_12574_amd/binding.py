@@ -87,6 +87,7 @@ _native = None       # _pycall, bound to the library: the calls of a token witho
 class _CtypesOnly:
     """In _pycall's place where it was not built for this interpreter: every call goes through ctypes."""
     prefill_group = decode_group = decode_group_ragged = qkv_rope = out_proj = staticmethod(lambda *args: None)
+    add_rmsnorm = linear_quantized = paged_append = paged_attn = staticmethod(lambda *args: None)
 
 
 def _load_native():
@@ -100,6 +101,9 @@ def _load_native():
         return _native
     _pycall.bind(*[C.cast(f, C.c_void_p).value for f in (L.hi_prefill_group, L.hi_decode_group, L.hi_decode_group_ragged,
                                                          L.hi_qkv_rope, L.hi_out_proj)], C.c_void_p)
+    serving = [getattr(L, name, None) for name in ("hi_add_rmsnorm", "hi_linear_quantized", "hi_paged_append", "hi_paged_attn")]
+    if None not in serving:
+        _pycall.bind_serving(*[C.cast(f, C.c_void_p).value for f in serving])
     _native = _pycall
     return _native
 
@@ -348,8 +352,11 @@ def hi_kv_dequantize(stream, packed_dev, n_rows, rows_dev, check: bool = True):
 
 def hi_add_rmsnorm(stream, x_dev, x_fp32, residual_dev, residual_fp32, weight_dev, n_rows, d, eps, residual_out_dev, out_dev,
                    check: bool = True):
-    st = lib().hi_add_rmsnorm(_stream(stream), _ptr(x_dev), x_fp32, _ptr(residual_dev), residual_fp32, _ptr(weight_dev), n_rows,
-                              d, eps, _ptr(residual_out_dev), _ptr(out_dev))
+    st = (_native or _load_native()).add_rmsnorm(stream, x_dev, x_fp32, residual_dev, residual_fp32, weight_dev, n_rows, d, eps,
+                                                 residual_out_dev, out_dev)
+    if st is None:
+        st = lib().hi_add_rmsnorm(_stream(stream), _ptr(x_dev), x_fp32, _ptr(residual_dev), residual_fp32, _ptr(weight_dev),
+                                  n_rows, d, eps, _ptr(residual_out_dev), _ptr(out_dev))
     if check and st != HI_OK:
         raise HiError(st, "hi_add_rmsnorm")
     return st
@@ -364,8 +371,11 @@ def hi_weight_quantize(stream, w_dev, n_out, n_in, codes_dev, scales_dev, zeros_
 
 def hi_linear_quantized(stream, x_dev, codes_dev, scales_dev, zeros_dev, n_rows, n_in, n_out, x_heads, y_heads, y_dev,
                         check: bool = True):
-    st = lib().hi_linear_quantized(_stream(stream), _ptr(x_dev), _ptr(codes_dev), _ptr(scales_dev), _ptr(zeros_dev), n_rows, n_in,
-                                   n_out, x_heads, y_heads, _ptr(y_dev))
+    st = (_native or _load_native()).linear_quantized(stream, x_dev, codes_dev, scales_dev, zeros_dev, n_rows, n_in, n_out, x_heads,
+                                                      y_heads, y_dev)
+    if st is None:
+        st = lib().hi_linear_quantized(_stream(stream), _ptr(x_dev), _ptr(codes_dev), _ptr(scales_dev), _ptr(zeros_dev), n_rows,
+                                       n_in, n_out, x_heads, y_heads, _ptr(y_dev))
     if check and st != HI_OK:
         raise HiError(st, "hi_linear_quantized")
     return st
@@ -375,6 +385,7 @@ def make_paged_cache(pages, scales, n_pages, n_kv_heads, page_rows, kv_bits=16) 
     """pages: [n_pages][n_kv_heads][2][page_rows][128] bf16 (kv_bits 16) or e4m3 (8); scales: fp32 without the last axis, or None."""
     c = hi_paged_cache(_ptr(pages), _ptr(scales), n_pages, n_kv_heads, page_rows, kv_bits)
     c._keepalive = (pages, scales)                    # the struct only holds addresses
+    c.address = C.addressof(c)                        # (its own, for the native marshalling)
     return c
 
 
@@ -382,13 +393,17 @@ def make_paged_batch(page_table, past_lens, row_starts, n_seqs, table_pages, n_r
     """page_table [n_seqs][table_pages], past_lens [n_seqs], row_starts [n_seqs + 1]: int32 on the device."""
     b = hi_paged_batch(_ptr(page_table), _ptr(past_lens), _ptr(row_starts), n_seqs, table_pages, n_rows, max_rows)
     b._keepalive = (page_table, past_lens, row_starts)
+    b.address = C.addressof(b)
     return b
 
 
 def hi_paged_append(stream, cache: hi_paged_cache, batch: hi_paged_batch, q_in_dev, k_in_dev, v_in_dev, in_fp32, n_q_heads,
                     rope_theta, q_scale, q_out_dev, check: bool = True):
-    st = lib().hi_paged_append(_stream(stream), cache, batch, _ptr(q_in_dev), _ptr(k_in_dev), _ptr(v_in_dev), in_fp32, n_q_heads,
-                               rope_theta, q_scale, _ptr(q_out_dev))
+    st = (_native or _load_native()).paged_append(stream, cache, batch, q_in_dev, k_in_dev, v_in_dev, in_fp32, n_q_heads, rope_theta,
+                                                  q_scale, q_out_dev)
+    if st is None:
+        st = lib().hi_paged_append(_stream(stream), cache, batch, _ptr(q_in_dev), _ptr(k_in_dev), _ptr(v_in_dev), in_fp32,
+                                   n_q_heads, rope_theta, q_scale, _ptr(q_out_dev))
     if check and st != HI_OK:
         raise HiError(st, "hi_paged_append")
     return st
@@ -404,8 +419,10 @@ def hi_paged_workspace_bytes(n_q_heads: int, n_kv_heads: int) -> int:
 
 def hi_paged_attn(stream, cache: hi_paged_cache, batch: hi_paged_batch, q_dev, n_q_heads, q_prescaled, out_dev, workspace_dev,
                   check: bool = True):
-    st = lib().hi_paged_attn(_stream(stream), cache, batch, _ptr(q_dev), n_q_heads, q_prescaled, _ptr(out_dev),
-                             _ptr(workspace_dev))
+    st = (_native or _load_native()).paged_attn(stream, cache, batch, q_dev, n_q_heads, q_prescaled, out_dev, workspace_dev)
+    if st is None:
+        st = lib().hi_paged_attn(_stream(stream), cache, batch, _ptr(q_dev), n_q_heads, q_prescaled, _ptr(out_dev),
+                                 _ptr(workspace_dev))
     if check and st != HI_OK:
         raise HiError(st, "hi_paged_attn")
     return st

@@ -16,7 +16,11 @@ decltype(&hi_decode_group) f_decode;
 decltype(&hi_decode_group_ragged) f_ragged;
 decltype(&hi_qkv_rope) f_qkv;
 decltype(&hi_out_proj) f_out;
-PyObject *s_data_ptr, *s_cuda_stream, *s_value, *c_void_p_type;
+decltype(&hi_add_rmsnorm) f_norm;
+decltype(&hi_linear_quantized) f_linear;
+decltype(&hi_paged_append) f_append;
+decltype(&hi_paged_attn) f_attn;
+PyObject *s_data_ptr, *s_cuda_stream, *s_value, *s_address, *c_void_p_type;
 
 // One call's arguments.  ok goes down at the first unusual one; a Python error (of a data_ptr, say) is kept and raised.
 struct Args {
@@ -56,6 +60,13 @@ struct Args {
   void* stream(Py_ssize_t i) {
     if (!ok || a[i] == Py_None || PyLong_Check(a[i])) return ok ? address(a[i]) : nullptr;
     return from(PyObject_GetAttr(a[i], s_cuda_stream));
+  }
+  template <class T>
+  const T* structure(Py_ssize_t i) {              // a ctypes structure that knows its own address
+    if (!ok || a[i] == Py_None || PyLong_Check(a[i])) { ok = false; return nullptr; }
+    PyObject* const got = PyObject_GetAttr(a[i], s_address);
+    if (!got) { PyErr_Clear(); ok = false; return nullptr; }
+    return (const T*)from(got);
   }
   hi_ctx* context(Py_ssize_t i) {
     if (!ok || a[i] == Py_None || PyLong_Check(a[i])) return ok ? (hi_ctx*)address(a[i]) : nullptr;
@@ -144,6 +155,70 @@ PyObject* out_proj(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return run(g, [&] { return f_out(s, x, w, hq, d, len, fp32, y); });
 }
 
+PyObject* add_rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!f_norm || n != 11) Py_RETURN_NONE;
+  Args g{a};
+  void *s = g.stream(0), *x = g.buffer(1);
+  const int32_t xf = g.int32(2);
+  void* r = g.buffer(3);
+  const int32_t rf = g.int32(4);
+  void* w = g.buffer(5);
+  const int32_t rows = g.int32(6), d = g.int32(7);
+  const float eps = (float)g.real(8);
+  void *ro = g.buffer(9), *out = g.buffer(10);
+  return run(g, [&] { return f_norm(s, x, xf, r, rf, w, rows, d, eps, ro, out); });
+}
+
+PyObject* linear_quantized(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!f_linear || n != 11) Py_RETURN_NONE;
+  Args g{a};
+  void *s = g.stream(0), *x = g.buffer(1), *c = g.buffer(2), *sc = g.buffer(3), *z = g.buffer(4);
+  const int32_t rows = g.int32(5), n_in = g.int32(6), n_out = g.int32(7), xh = g.int32(8), yh = g.int32(9);
+  void* y = g.buffer(10);
+  return run(g, [&] { return f_linear(s, x, c, sc, z, rows, n_in, n_out, xh, yh, y); });
+}
+
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!f_append || n != 11) Py_RETURN_NONE;
+  Args g{a};
+  void* s = g.stream(0);
+  const hi_paged_cache* c = g.structure<hi_paged_cache>(1);
+  const hi_paged_batch* b = g.structure<hi_paged_batch>(2);
+  void *q = g.buffer(3), *k = g.buffer(4), *v = g.buffer(5);
+  const int32_t fp32 = g.int32(6), heads = g.int32(7);
+  const double theta = g.real(8);
+  const float scale = (float)g.real(9);
+  void* out = g.buffer(10);
+  return run(g, [&] { return f_append(s, c, b, q, k, v, fp32, heads, theta, scale, out); });
+}
+
+PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!f_attn || n != 8) Py_RETURN_NONE;
+  Args g{a};
+  void* s = g.stream(0);
+  const hi_paged_cache* c = g.structure<hi_paged_cache>(1);
+  const hi_paged_batch* b = g.structure<hi_paged_batch>(2);
+  void* q = g.buffer(3);
+  const int32_t heads = g.int32(4), pre = g.int32(5);
+  void *out = g.buffer(6), *ws = g.buffer(7);
+  return run(g, [&] { return f_attn(s, c, b, q, heads, pre, out, ws); });
+}
+
+// bind_serving(add_rmsnorm, linear_quantized, paged_append, paged_attn): the functions' addresses
+PyObject* bind_serving(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 4) { PyErr_SetString(PyExc_TypeError, "bind_serving takes four addresses"); return nullptr; }
+  void* p[4];
+  for (int i = 0; i < 4; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (!p[i]) { if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address"); return nullptr; }
+  }
+  f_norm = (decltype(f_norm))p[0];
+  f_linear = (decltype(f_linear))p[1];
+  f_append = (decltype(f_append))p[2];
+  f_attn = (decltype(f_attn))p[3];
+  Py_RETURN_NONE;
+}
+
 // bind(prefill_group, decode_group, decode_group_ragged, qkv_rope, out_proj, ctypes.c_void_p): the functions' addresses
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 6) { PyErr_SetString(PyExc_TypeError, "bind takes five addresses and a type"); return nullptr; }
@@ -169,6 +244,11 @@ PyMethodDef methods[] = {
     {"decode_group_ragged", (PyCFunction)(void (*)(void))decode_group_ragged, METH_FASTCALL, nullptr},
     {"qkv_rope", (PyCFunction)(void (*)(void))qkv_rope, METH_FASTCALL, nullptr},
     {"out_proj", (PyCFunction)(void (*)(void))out_proj, METH_FASTCALL, nullptr},
+    {"bind_serving", (PyCFunction)(void (*)(void))bind_serving, METH_FASTCALL, nullptr},
+    {"add_rmsnorm", (PyCFunction)(void (*)(void))add_rmsnorm, METH_FASTCALL, nullptr},
+    {"linear_quantized", (PyCFunction)(void (*)(void))linear_quantized, METH_FASTCALL, nullptr},
+    {"paged_append", (PyCFunction)(void (*)(void))paged_append, METH_FASTCALL, nullptr},
+    {"paged_attn", (PyCFunction)(void (*)(void))paged_attn, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -178,6 +258,7 @@ PyMODINIT_FUNC PyInit__pycall(void) {
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
   s_value = PyUnicode_InternFromString("value");
-  if (!s_data_ptr || !s_cuda_stream || !s_value) return nullptr;
+  s_address = PyUnicode_InternFromString("address");
+  if (!s_data_ptr || !s_cuda_stream || !s_value || !s_address) return nullptr;
   return PyModule_Create(&module_def);
 }

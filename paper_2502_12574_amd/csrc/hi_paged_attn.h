@@ -14,9 +14,9 @@ constexpr int kPagedPieceFloats = 16 * kPartialFloats;
 
 // hi_paged_chunk.hip: two workgroups of 128 rows a compute unit; a block that is cut leaves an image of its state (64 O^T accumulators, m
 // and l for each of 256 lanes) for each piece.  Pieces have at least the tiles of all blocks / (2 x 512), so there are at most twice
-// as many images as that.
+// as many images as that (and a few, as that share is worked out in fp32).
 constexpr int kPagedSlots = 512;
-constexpr int kPagedMostImages = 4 * kPagedSlots;
+constexpr int kPagedMostImages = 4 * kPagedSlots + 16;
 constexpr int kPagedImageFloats = 66 * 256;
 
 struct PagedAttnArgs {
@@ -25,7 +25,7 @@ struct PagedAttnArgs {
   int q_heads, group;
   int positions, by_group;       // positions of a block; 65536 / group, rounded up
   float c;                       // what a score is multiplied by before the power of two
-  int* arrivals; float* pieces; float* images;   // in the workspace
+  int* arrivals; int* plan; float* pieces; float* images;   // in the workspace
 };
 
 hi_status launch_paged_decode(void* stream, const PagedAttnArgs& a);

@@ -5,8 +5,8 @@ namespace hi {
 
 namespace {
 
-// The workspace: arrival counts, then either the pieces of the one kernel or the images of the other.
-constexpr int kArrivalBytes = kPagedArrivals * 4;
+// The workspace: arrival counts, the length of a piece, then either the pieces of the one kernel or the images of the other.
+constexpr int kArrivalBytes = kPagedArrivals * 4 + 256;
 
 }  // namespace
 
@@ -41,6 +41,7 @@ extern "C" hi_status hi_paged_attn(void* stream, const hi_paged_cache* cache, co
   a.q_heads = n_q_heads; a.group = group;
   a.c = softmax_scale_log2(q_prescaled != 0);
   a.arrivals = (int*)workspace_dev;
+  a.plan = a.arrivals + kPagedArrivals;
   a.pieces = a.images = (float*)((char*)workspace_dev + kArrivalBytes);
   a.by_group = (65536 + group - 1) / group;
   a.positions = 16 / group;

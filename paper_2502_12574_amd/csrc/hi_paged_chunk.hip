@@ -85,10 +85,53 @@ __device__ __forceinline__ int pieces_of(int tiles, uint32_t piece) { return (in
 // What a workgroup does: its block, and the tiles [t0, t1) of it; pieces of the block, the block's first image and the distance of the
 // next piece's (number: the workgroup's, or with MERGE the block's).
 struct ChunkWork { int seq, kv, row0, rows, tiles, t0, t1, sees, len, pieces, piece, image, next_image; bool any; };
+// The tiles of a piece: whole blocks, or pieces of an even share of the tiles of all blocks over one round of workgroups, an eighth or a
+// quarter more of it (an even share often leaves a few pieces for a round of their own), or over two rounds.  A workgroup costs 6 tiles
+// to begin and to end, a merge 3 and one for every 70 images, and a round ends with its longest piece unless the short ones that
+// follow fill its gaps.  0: there is nothing to do.
+// 384 rows behind 8000, 96 blocks of 131 tiles: 89 us with even shares (576 pieces), 79 with an eighth more (480).
+__device__ __forceinline__ uint32_t chunk_piece(const PagedAttnArgs& a, int lane) {
+  const int S = a.seqs.n_seqs;
+  float tiles = 0.f, blocks = 0.f, total = 0.f, longest = 0.f;     // (as near as is needed)
+  auto look = [&](int s0) __attribute__((always_inline)) {
+    const SeqBlocks b = seq_blocks(a, s0 + lane < S ? paged_seq_of(a.seqs, s0 + lane) : PagedSeq{0, 0, 0});
+    tiles = b.blocks > 0 ? (float)b.tiles : 0.f;
+    blocks = (float)b.blocks * (float)a.pool.heads;
+  };
+  for (int s0 = 0; s0 < S; s0 += 64) {
+    look(s0);
+    total += over_wave(tiles * blocks, op_add);
+    longest = fmaxf(longest, over_wave(tiles, op_max));
+  }
+  if (!(total >= 1.f) || total > 2.1e9f) return 0;                 // (sequences that overlap could overflow the count)
+  float best = longest, least = 0.f;
+  const float share = total * (1.f / kPagedSlots);
+#pragma unroll
+  for (int i = 0; i < 6; ++i) {
+    constexpr float kShares[6] = {0.f, 1.f, 1.125f, 1.25f, 0.5f, 0.5625f};
+    const float size = i == 0 ? longest : fmaxf(ceilf(share * kShares[i]), 4.f);
+    if (i > 0 && size >= longest) continue;
+    const float by_size = __builtin_amdgcn_rcpf(size);
+    float n = 0.f;
+    for (int s0 = 0; s0 < S; s0 += 64) {
+      if (S > 64) look(s0);
+      n += over_wave(ceilf(tiles * by_size - 1e-3f) * blocks, op_add);
+    }
+    const float rounds = ceilf(n * (1.f / kPagedSlots)) * (size + 6.f), filled = (total + 6.f * n) * (1.f / kPagedSlots) + size;
+    const float cost = fminf(rounds, filled) + (i == 0 ? 0.f : 3.f + n * (1.f / 70.f));
+    if (i == 0 || cost < least) {
+      least = cost;
+      best = size;
+    }
+  }
+  return __builtin_amdgcn_readfirstlane((uint32_t)best);
+}
+
 template <bool MERGE>
-__device__ __forceinline__ ChunkWork chunk_work(const PagedAttnArgs& a, int number, int lane) {
+__device__ __forceinline__ ChunkWork chunk_work(const PagedAttnArgs& a, uint32_t piece, int number, int lane) {
   ChunkWork w;
   w.any = false;
+  if (piece == 0) return w;
   const int S = a.seqs.n_seqs, H = a.pool.heads;
   PagedSeq q = {0, 0, 0};
   SeqBlocks sb = {0, 0};
@@ -96,44 +139,10 @@ __device__ __forceinline__ ChunkWork chunk_work(const PagedAttnArgs& a, int numb
     q = s0 + lane < S ? paged_seq_of(a.seqs, s0 + lane) : PagedSeq{0, 0, 0};
     sb = seq_blocks(a, q);
   };
-  uint32_t total = 0;
-  int longest = 1;
-  float about = 0.f;                             // (a batch whose sequences overlap could overflow the count)
-  for (int s0 = 0; s0 < S; s0 += 64) {
-    look(s0);
-    total += __builtin_amdgcn_readlane(sum_wave(sb.tiles * sb.blocks * H), 63);
-    about += over_wave((float)sb.tiles * (float)sb.blocks * (float)H, op_add);
-    const int most = (int)over_wave((float)(sb.blocks > 0 ? sb.tiles : 0), op_max);      // (as near as is needed)
-    longest = most > longest ? most : longest;
-  }
-  if (about > 2.1e9f) return w;
-  // Whole blocks, or pieces of the tiles of all blocks over one or two rounds: a workgroup costs 6 tiles to begin and to end, a merge 3
-  // and one for every 70 images, and a round ends with its longest piece unless the short ones that follow fill its gaps.
-  uint32_t piece = longest;
-  float least = 0.f;
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    uint32_t size = i == 0 ? (uint32_t)longest : (total + i * kPagedSlots - 1) / (i * kPagedSlots);
-    size = size < 4 ? 4 : size;
-    if (i > 0 && size >= (uint32_t)longest) break;
-    int n = 0;
-    for (int s0 = 0; s0 < S; s0 += 64) {
-      if (S > 64) look(s0);
-      n += __builtin_amdgcn_readlane(sum_wave(pieces_of(sb.tiles, size) * sb.blocks * H), 63);
-    }
-    const float rounds = (float)((n + kPagedSlots - 1) / kPagedSlots) * ((float)size + 6.f);
-    const float filled = ((float)total + 6.f * (float)n) * (1.f / kPagedSlots) + (float)size;
-    const float cost = fminf(rounds, filled) + (i == 0 ? 0.f : 3.f + (float)n * (1.f / 70.f));
-    if (i == 0 || cost < least) {
-      least = cost;
-      piece = size;
-    }
-  }
-  piece = __builtin_amdgcn_readfirstlane(piece);
   // the sequence that has the number; images: those of the sequences before it
   int before = 0, images = 0, seq = 0, n_blocks = 0, k = 1;
   for (int s0 = 0; s0 < S; s0 += 64) {
-    if (S > 64) look(s0);
+    look(s0);
     const int cut = pieces_of(sb.tiles, piece), here = sb.blocks * H * (MERGE ? 1 : cut), kept = cut > 1 ? sb.blocks * H * cut : 0;
     const int upto = sum_wave(here), images_upto = sum_wave(kept);
     const int n = __popcll(__builtin_amdgcn_ballot_w64(before + upto <= number));
@@ -200,7 +209,9 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds_raw[kLds<BITS>];
   lds_char* const lds = (lds_char*)lds_raw;
   const int lane = lane_id(), wave = wave_id(), hl = lane >> 5, col = lane & 31;
-  const ChunkWork w = chunk_work<false>(a, blockIdx.x, lane);
+  const uint32_t size = chunk_piece(a, lane);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.plan = (int)size;        // for the merge
+  const ChunkWork w = chunk_work<false>(a, size, blockIdx.x, lane);
   if (!w.any || w.t0 >= w.t1) return;
   const int n = w.t1 - w.t0;
   const int* const table = a.seqs.table + (int64_t)w.seq * a.seqs.table_pages;
@@ -474,7 +485,7 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
 // Joins the pieces of a block: a workgroup for each 32 dims of it, in the lanes of the kernel above.
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   const int lane = lane_id(), wave = wave_id(), db = blockIdx.y;
-  const ChunkWork w = chunk_work<true>(a, blockIdx.x, lane);
+  const ChunkWork w = chunk_work<true>(a, (uint32_t)*a.plan, blockIdx.x, lane);
   if (!w.any || w.pieces == 1 || 32 * wave >= w.rows * a.group) return;
   const LaneRow mine = lane_row(a, w, 32 * wave + (lane & 31));
   const float* const images = a.images + (int64_t)w.image * kPagedImageFloats + threadIdx.x;

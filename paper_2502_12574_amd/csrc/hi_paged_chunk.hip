@@ -10,7 +10,7 @@
 // A wavefront holds 32 rows.  S^T = K Q^T (32x32x16 tiles) leaves a row in one lane column: its running maximum and sum are per lane,
 // and the weights, rounded to bf16, are the B operand of O^T += V^T P^T as they lie.  bf16 tiles go to LDS by direct loads; rows of
 // 8 bits pass through registers, where they become bf16 (exactly) once for the whole workgroup, and their scales multiply scores
-// and weights in fp32.  Two workgroups a compute unit hide each other's softmax.
+// and weights in fp32 (that of a K row in the operation that takes the reference off its scores: it is brought along times c).  Two workgroups a compute unit hide each other's softmax.
 #include "hi_paged_attn.h"
 
 namespace hi {
@@ -21,9 +21,10 @@ constexpr int kRows = 128;                       // rows of a block
 constexpr int kTileRows = 64;
 constexpr int kTileBytes = kTileRows * kRowBytes;   // 16 KiB of K (or V), bf16
 constexpr int kStageBytes = 2 * kTileBytes;
-constexpr int kScalesAt = 2 * kStageBytes;       // [stage][K|V][64] fp32
+constexpr int kScalesAt = 2 * kStageBytes;       // [stage][K|V][64] fp32, then 64 ones
+constexpr int kOnesAt = kScalesAt + 2 * 2 * kTileRows * 4;
 constexpr float kSumLimit = 4096.f;
-template <int BITS> constexpr int kLds = kScalesAt + (BITS == 8 ? 2 * 2 * kTileRows * 4 : 0);
+template <int BITS> constexpr int kLds = BITS == 8 ? kOnesAt + kTileRows * 4 : kScalesAt;
 
 typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
@@ -298,10 +299,12 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
       put((ka ^ 128) + 8 * kRowBytes, k_hi);
       put(va, v_lo);
       put(va + 8 * kRowBytes, v_hi);
-      if (lane < 32) *(lds_float*)(lds + kScalesAt + ((stage * 2 + (lane >> 4)) * kTileRows + 16 * wave + (lane & 15)) * 4) = row_scale;
+      if (lane < 32) *(lds_float*)(lds + kScalesAt + ((stage * 2 + (lane >> 4)) * kTileRows + 16 * wave + (lane & 15)) * 4) = lane < 16 ? row_scale * a.c : row_scale;
     }
   };
   fetch(0, 0);
+  if (BITS == 8 && threadIdx.x < kTileRows) *(lds_float*)(lds + kOnesAt + threadIdx.x * 4) = 1.f;
+  const float unit = BITS == 8 ? 1.f : a.c;      // what scores and maxima are multiplied by before the power of two
 
   // rows that a piece's tiles lack because their page is not there: looked for once
   bool holes = false;
@@ -370,18 +373,20 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
       __builtin_amdgcn_sched_barrier(0);
     }
     lds_char* const sc = lds + kScalesAt + stage * 2 * kTileRows * 4 + 16 * hl;
-    if constexpr (BITS == 8) {
-#pragma unroll
-      for (int sb = 0; sb < 2; ++sb)
-#pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          const f32x4 f = *(lds_f32x4*)(sc + (32 * sb + 8 * q4) * 4);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) s[sb][4 * q4 + r] *= f[r];
-        }
-    }
     const bool hides = key0 + kTileRows - 1 > w.sees;
+    lds_char* by_key = sc;                       // what the scores are still to be multiplied by
     if (hides || holes) {
+      if constexpr (BITS == 8) {
+#pragma unroll
+        for (int sb = 0; sb < 2; ++sb)
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            const f32x4 f = *(lds_f32x4*)(sc + (32 * sb + 8 * q4) * 4);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[sb][4 * q4 + r] *= f[r];
+          }
+        by_key = lds + kOnesAt + 16 * hl;
+      }
       uint64_t shown = lim - key0 >= 63 ? ~0ull : lim < key0 ? 0ull : (2ull << (lim - key0)) - 1;
       if (holes) {
 #pragma unroll
@@ -410,8 +415,17 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           float p[8];
+          if constexpr (BITS == 8) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) p[e] = fast_exp2(__builtin_fmaf(s[sb][8 * u + e], a.c, -mc));
+            for (int h = 0; h < 2; ++h) {
+              const f32x4 f = *(lds_f32x4*)(by_key + (32 * sb + 16 * u + 8 * h) * 4);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) p[4 * h + r] = fast_exp2(__builtin_fmaf(s[sb][8 * u + 4 * h + r], f[r], -mc));
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[e] = fast_exp2(__builtin_fmaf(s[sb][8 * u + e], a.c, -mc));
+          }
           lq[2 * sb + u] = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
           if constexpr (BITS == 8) {
 #pragma unroll
@@ -432,21 +446,26 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
       for (int i = 0; i < A; ++i) read_v(i);
       __builtin_amdgcn_sched_barrier(0);
     }
-    float sum = weights(st.m > kNegBig ? st.m * a.c : 0.f);
+    float sum = weights(st.m > kNegBig ? st.m * unit : 0.f);
     if (__builtin_amdgcn_ballot_w64(!(sum <= kSumLimit) || st.m == kNegBig) != 0) {       // also true for NaN
-      float mx = s[0][0];
+      float mx = kNegBig;
 #pragma unroll
       for (int sb = 0; sb < 2; ++sb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[sb][r]);
-      const float m_new = fmaxf(st.m, both_halves(mx, true)), alpha = fast_exp2((st.m - m_new) * a.c);
+        for (int q4 = 0; q4 < 4; ++q4) {
+          f32x4 f = {1.f, 1.f, 1.f, 1.f};
+          if constexpr (BITS == 8) f = *(lds_f32x4*)(by_key + (32 * sb + 8 * q4) * 4);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) mx = fmaxf(mx, BITS == 8 ? s[sb][4 * q4 + r] * f[r] : s[sb][4 * q4 + r]);
+        }
+      const float m_new = fmaxf(st.m, both_halves(mx, true)), alpha = fast_exp2((st.m - m_new) * unit);
       st.l *= alpha;
 #pragma unroll
       for (int db = 0; db < 4; ++db)
 #pragma unroll
         for (int r = 0; r < 16; ++r) st.o[db][r] *= alpha;
       st.m = m_new;
-      sum = weights(st.m > kNegBig ? st.m * a.c : 0.f);            // (a row that has seen nothing yet adds weights of zero)
+      sum = weights(st.m > kNegBig ? st.m * unit : 0.f);           // (a row that has seen nothing yet adds weights of zero)
     }
     st.l += sum;
     __builtin_amdgcn_sched_barrier(0);
@@ -494,6 +513,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   auto left = [&](int p) __attribute__((always_inline)) {
     return (uint64_t)w.tiles * (uint32_t)p / (uint32_t)w.pieces < (uint64_t)w.tiles * (uint32_t)(p + 1) / (uint32_t)w.pieces;
   };
+  const float unit = a.pool.bits == 8 ? 1.f : a.c;
   float m = kNegBig, l = 0.f;
   f32x16 o;
 #pragma unroll
@@ -516,14 +536,14 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
         for (int r = 0; r < 16; ++r) po[i][r] = x[(db * 16 + r) * 256];
       }
     }
-    const float mn = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), m), f = fast_exp2((m - mn) * a.c);
+    const float mn = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), m), f = fast_exp2((m - mn) * unit);
     m = mn;
     l *= f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[r] *= f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float e = fast_exp2((pm[i] - m) * a.c);
+      const float e = fast_exp2((pm[i] - m) * unit);
       l += e * pl[i];
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[r] += e * po[i][r];

@@ -7,7 +7,7 @@
 // kPagedStart tiles more: its first loads and its merge are not hidden by anything); where there are so few
 // that every block can be cut into equal pieces of at most a run without more pieces than workgroups, a workgroup takes such a piece
 // instead.  Every workgroup finds its part from the lengths themselves, so nothing is planned on the host and a captured launch
-// follows them.  A block that lies in several parts is merged by the workgroup that finishes last: by sixteens, then the sixteens.
+// follows them.  A block that lies in several parts is merged by the workgroup that finishes last: 16 or 32 parts at a time, then those.
 //
 // A workgroup's 4 wavefronts take the tiles of a block in turn, each with a private LDS ring of direct-to-LDS loads and no barrier
 // in the loop.  The rows ride as the 16 columns of small MFMA tiles: S^T = K Q^T, O^T += V^T P^T.  8-bit rows are expanded to bf16
@@ -37,7 +37,6 @@ template <int BITS> constexpr int kWaveLds = Ring<BITS>::kSlot * Ring<BITS>::kSl
 constexpr int kPiece = kCols * kPartialFloats;                  // floats of a piece: O[128], m, l for each column
 template <int BITS> constexpr int kLds = 4 * kWaveLds<BITS> > 4 * kPiece * 4 ? 4 * kWaveLds<BITS> : 4 * kPiece * 4;
 static_assert(kLds<16> <= 159 * 1024 && kLds<8> <= 159 * 1024, "a workgroup's LDS");
-constexpr int kFan = 16;                                        // pieces that are merged at once
 
 // 4 bytes per lane, global -> LDS at lds_uniform + 4 * lane
 __device__ __forceinline__ void g2lds4_s(const char* sbase, uint32_t voff, uint32_t lds_uniform_addr) {
@@ -268,42 +267,51 @@ __device__ __forceinline__ void write_out(const PagedAttnArgs& a, int kv, int ro
   *(uint32_t*)(a.out + ((int64_t)(kv * a.group + g) * a.seqs.n_rows + row0 + pos) * kHeadDim + d) = pack_bf16(o.x * inv, o.y * inv);
 }
 
-// A merge of up to 16 pieces, piece_at(i) being where piece i lies: wavefront w takes every fourth, for four columns at a time (all 32
-// loads of them under way together), and leaves its sums in LDS.
-template <class At>
-__device__ __forceinline__ void gather_pieces(int n, At piece_at, int cols, float* red, float c, int lane, int wave) {
-  static_assert(kFan == 16, "four pieces a wavefront");
-  for (int c0 = 0; c0 < cols; c0 += 4) {
-    float2 ml[4][4], x[4][4];
+// A merge of up to 4 P pieces, piece_at(i) being where piece i lies: wavefront w takes every fourth, for N columns from c0 on (all their
+// loads under way together), and leaves its sums in LDS.
+template <int P, int N, class At>
+__device__ __forceinline__ void gather_columns(int n, At piece_at, int c0, int cols, float* red, float c, int lane, int wave) {
+  float2 ml[P][N], x[P][N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < P; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int p = wave + 4 * i;
-        ml[i][j] = make_float2(kNegBig, 0.f);
-        x[i][j] = make_float2(0.f, 0.f);
-        if (p < n && c0 + j < cols) {
-          const float* const at = piece_at(p) + (c0 + j) * kPartialFloats;
-          ml[i][j] = load_shared2(at + kHeadDim);
-          x[i][j] = load_shared2(at + 2 * lane);
-        }
-      }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float m = fmaxf(fmaxf(ml[0][j].x, ml[1][j].x), fmaxf(ml[2][j].x, ml[3][j].x));
-      float l = 0.f;
-      float2 o = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float e = fast_exp2((ml[i][j].x - m) * c);
-        l += e * ml[i][j].y; o.x += e * x[i][j].x; o.y += e * x[i][j].y;
-      }
-      if (c0 + j < cols) {
-        float* const to = red + wave * kPiece + (c0 + j) * kPartialFloats;
-        *(float2*)(to + 2 * lane) = o;
-        if (lane == 0) *(float2*)(to + kHeadDim) = make_float2(m, l);
+    for (int j = 0; j < N; ++j) {
+      const int p = wave + 4 * i;
+      ml[i][j] = make_float2(kNegBig, 0.f);
+      x[i][j] = make_float2(0.f, 0.f);
+      if (p < n && c0 + j < cols) {
+        const float* const at = piece_at(p) + (c0 + j) * kPartialFloats;
+        ml[i][j] = load_shared2(at + kHeadDim);
+        x[i][j] = load_shared2(at + 2 * lane);
       }
     }
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    float m = ml[0][j].x, l = 0.f;
+#pragma unroll
+    for (int i = 1; i < P; ++i) m = fmaxf(m, ml[i][j].x);
+    float2 o = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const float e = fast_exp2((ml[i][j].x - m) * c);
+      l += e * ml[i][j].y; o.x += e * x[i][j].x; o.y += e * x[i][j].y;
+    }
+    if (c0 + j < cols) {
+      float* const to = red + wave * kPiece + (c0 + j) * kPartialFloats;
+      *(float2*)(to + 2 * lane) = o;
+      if (lane == 0) *(float2*)(to + kHeadDim) = make_float2(m, l);
+    }
+  }
+}
+// How many pieces are merged at once: the loads of 32 of up to 4 columns, or of 16 of 8, fit the registers.
+__device__ __forceinline__ int fan_of(int cols) { return cols <= 4 ? 32 : 16; }
+template <class At>
+__device__ __forceinline__ void gather_pieces(int n, At piece_at, int cols, float* red, float c, int lane, int wave) {
+  if (cols <= 4) {
+    if (n <= 16) gather_columns<4, 4>(n, piece_at, 0, cols, red, c, lane, wave);
+    else gather_columns<8, 4>(n, piece_at, 0, cols, red, c, lane, wave);
+  } else {
+    for (int c0 = 0; c0 < cols; c0 += 8) gather_columns<4, 8>(n, piece_at, c0, cols, red, c, lane, wave);
   }
 }
 
@@ -534,7 +542,8 @@ __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
     } else {
       const int first = (begin + start) / step, last = (done - 1) / step, me = blockIdx.x;
       auto piece_of = [&](int p) __attribute__((always_inline)) { return a.pieces + (int64_t)(2 * p + (p == first)) * kPiece; };
-      const int fan = (me - first) / kFan, lead = first + fan * kFan, n_fan = last - lead + 1 < kFan ? last - lead + 1 : kFan, fans = (last - first) / kFan + 1;
+      const int most_at_once = fan_of(cols), fan = (me - first) / most_at_once, lead = first + fan * most_at_once;
+      const int n_fan = last - lead + 1 < most_at_once ? last - lead + 1 : most_at_once, fans = (last - first) / most_at_once + 1;
       put(piece_of(me));
       // (of a run in which one block ends and another begins, each has a count of its own)
       if (last_of(a.arrivals + (fan == 0 ? 0 : kPagedRuns) + lead, n_fan)) {
@@ -542,7 +551,7 @@ __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
         __syncthreads();
         put(fans == 1 ? nullptr : piece_of(lead));
         if (fans > 1 && last_of(a.arrivals + 2 * kPagedRuns + first, fans)) {
-          gather_pieces(fans, [&](int p) __attribute__((always_inline)) { return piece_of(first + p * kFan); }, cols, red, a.c, lane, wave);
+          gather_pieces(fans, [&](int p) __attribute__((always_inline)) { return piece_of(first + p * most_at_once); }, cols, red, a.c, lane, wave);
           __syncthreads();
           put(nullptr);
         }
@@ -552,7 +561,7 @@ __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
     at = begin + u1;
   }
 }
-static_assert(kPagedRuns <= kFan * kFan, "two levels of merges");
+static_assert(kPagedRuns <= 16 * 16, "two levels of merges");
 
 template <int BITS>
 hi_status decode_go(void* stream, const PagedAttnArgs& a) {

@@ -469,8 +469,9 @@ typedef struct hi_paged_batch {
  *   for the next one.  Calls that may overlap in time need workspaces of their own, as do captured graphs that may.
  *   A row's sums may be cut differently when batch or hint change; the same call gives the same bits.
  * All buffers 16-byte aligned, the arrays of the batch 4-byte; cache and batch are HOST structs, read before the call returns;
- * n_seqs = 0 or n_rows = 0 does nothing.  Errors: HI_ERR_ARG, HI_ERR_UNSUPPORTED, HI_ERR_RANGE (a batch whose size, times
- * the length of the table, cannot be counted in 31 bits of 16-row blocks), HI_ERR_HIP.
+ * n_seqs = 0 or n_rows = 0 does nothing.  Errors: HI_ERR_ARG, HI_ERR_UNSUPPORTED, HI_ERR_RANGE (a table of more
+ * than 2^30 rows, more than 65535 query heads, or more work than the kernels count: 2e9 tiles of 32 keys, all sequences of the
+ * batch taken as long as the table), HI_ERR_HIP.
  */
 hi_status hi_paged_append(void* stream, const hi_paged_cache* cache, const hi_paged_batch* batch, const void* q_in_dev,
                           const void* k_in_dev, const void* v_in_dev, int32_t in_fp32, int32_t n_q_heads, double rope_theta,

@@ -19,7 +19,8 @@ hi_status paged_arguments(const hi_paged_cache* cache, const hi_paged_batch* bat
   if (!aligned_to(batch->page_table, 4) || !aligned_to(batch->past_lens, 4) || !aligned_to(batch->row_starts, 4)) { set_last_error("%s: batch arrays must be 4-byte aligned", what); return HI_ERR_ARG; }
   int shift = 4;
   while ((1 << shift) < r) ++shift;
-  if (((int64_t)batch->table_pages << shift) > 0x7FFFFFFF) { set_last_error("%s: a table of more than 2^31 - 1 rows", what); return HI_ERR_RANGE; }
+  // (rows, and the ends of tiles behind the last one, are counted in 32 bits)
+  if (((int64_t)batch->table_pages << shift) > (1 << 30)) { set_last_error("%s: a table of more than 2^30 rows", what); return HI_ERR_RANGE; }
   pool = {(char*)cache->pages, (float*)cache->scales, cache->n_pages, cache->n_kv_heads, shift, cache->kv_bits};
   seqs = {batch->page_table, batch->past_lens, batch->row_starts, batch->n_seqs, batch->table_pages, batch->n_rows};
   return HI_OK;
@@ -85,7 +86,7 @@ template <bool FP32, int ROWS>
 __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
   static_assert(ROWS <= kAppendMostRows, "a wavefront looks each row up");
   __shared__ float2 turn[ROWS][64];
-  __shared__ int place[ROWS][3];                // position (-1: no sequence has the row), page (-1: none), row of the page
+  __shared__ int place[ROWS][3];                // whether a sequence has the row, page (-1: none), row of the page
   const int t0 = blockIdx.x * ROWS, lane = lane_id(), wave = wave_id();
   const int H = a.pool.heads, heads = a.q_heads + 2 * H, tasks = heads * ROWS;
   const int c = threadIdx.x & 7;
@@ -109,24 +110,27 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
     int before = 0;                             // sequences that begin at t or before it
     for (int s = lane; s - lane < a.seqs.n_seqs; s += 64)
       before += __popcll(__builtin_amdgcn_ballot_w64(s < a.seqs.n_seqs && a.seqs.starts[s] <= t));
-    int pos = -1, page = -1;
+    bool has = false;
+    uint32_t pos = 0;                           // (of two numbers below 2^31: up to 2^32)
+    int page = -1;
     if (before > 0 && t < a.seqs.n_rows) {
       const PagedSeq q = paged_seq_of(a.seqs, before - 1);
-      if (t >= q.first && t < q.first + q.rows) pos = q.past + (t - q.first) >= 0 ? q.past + (t - q.first) : -1;
-      if (pos >= 0 && (pos >> a.pool.shift) < a.seqs.table_pages) {
+      has = t >= q.first && t < q.first + q.rows;
+      pos = (uint32_t)q.past + (uint32_t)(t - q.first);
+      if (has && (pos >> a.pool.shift) < (uint32_t)a.seqs.table_pages) {
         page = a.seqs.table[(int64_t)(before - 1) * a.seqs.table_pages + (pos >> a.pool.shift)];
         if (page >= a.pool.n_pages) page = -1;
       }
     }
-    if (a.rotate && pos >= 0) {
+    if (a.rotate && has) {
       double s, co;
       sincos((double)pos * a.f.inv[lane], &s, &co);
       turn[wave][lane] = make_float2((float)co, (float)s);
     }
     if (lane == 0) {
-      place[wave][0] = pos;
+      place[wave][0] = has;
       place[wave][1] = page;
-      place[wave][2] = pos & ((1 << a.pool.shift) - 1);
+      place[wave][2] = (int)(pos & ((1u << a.pool.shift) - 1));
     }
   }
   __syncthreads();
@@ -141,8 +145,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
       lo.load(src, at);
       hi.load(src, at + 64);
     }
-    const int pos = place[r][0], page = place[r][1];
-    if (pos < 0) continue;                      // (the 8 lanes of a row go the same way)
+    const int page = place[r][1];
+    if (!place[r][0]) continue;                 // (the 8 lanes of a row go the same way)
     if (a.rotate && head < a.q_heads + H) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {

@@ -19,10 +19,13 @@ constexpr int kPagedSlots = 512;
 constexpr int kPagedMostImages = 4 * kPagedSlots + 16;
 constexpr int kPagedImageFloats = 66 * 256;
 
+// Tiles (and starts) of all blocks, in 31 bits with something to spare for the kernels' fp32 estimates of it.
+constexpr float kPagedMostTiles = 2.0e9f;
+
 struct PagedAttnArgs {
   PagedPool pool; PagedSeqs seqs;
   const uint16_t* q; uint16_t* out;
-  int q_heads, group;
+  int group;
   int positions, by_group;       // positions of a block; 65536 / group, rounded up
   float c;                       // what a score is multiplied by before the power of two
   int* arrivals; int* plan; float* pieces; float* images;   // in the workspace

@@ -35,28 +35,27 @@ extern "C" hi_status hi_paged_attn(void* stream, const hi_paged_cache* cache, co
   if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads != 0 || (q_prescaled != 0 && q_prescaled != 1)) { set_last_error("paged attention: bad shape"); return HI_ERR_ARG; }
   const int group = n_q_heads / cache->n_kv_heads;
   if (group > 16) { set_last_error("paged attention: at most 16 query heads a KV head"); return HI_ERR_UNSUPPORTED; }
+  // (the scales of all heads of a page lie within 32 bits of bytes)
   if (n_q_heads > 65535) { set_last_error("paged attention: too many heads"); return HI_ERR_RANGE; }
   if (batch->n_seqs == 0 || batch->n_rows == 0) return HI_OK;
   a.q = (const uint16_t*)q_dev; a.out = (uint16_t*)out_dev;
-  a.q_heads = n_q_heads; a.group = group;
+  a.group = group;
   a.c = softmax_scale_log2(q_prescaled != 0);
   a.arrivals = (int*)workspace_dev;
   a.plan = a.arrivals + kPagedArrivals;
   a.pieces = a.images = (float*)((char*)workspace_dev + kArrivalBytes);
   a.by_group = (65536 + group - 1) / group;
-  a.positions = 16 / group;
-  // tiles of 16 rows, at the table's full length, have to be countable in 31 bits
-  const int64_t table_rows = (int64_t)batch->table_pages << a.pool.shift;
-  const int64_t blocks16 = (int64_t)batch->n_seqs + batch->n_rows / a.positions;
-  if ((double)blocks16 * (double)ceil_div(table_rows, 16) * (double)cache->n_kv_heads > 2147483647.0) {
+  const bool few = (int64_t)batch->max_rows * group <= 16;
+  a.positions = (few ? 16 : 128) / group;
+  // Blocks of all sequences: each but the last of a sequence is full, and each has a row.  Their tiles, at the table's full length, have
+  // to be countable, and there can be no more workgroups than 2^32 lanes.
+  const int64_t table_rows = (int64_t)batch->table_pages << a.pool.shift, most = batch->n_rows / a.positions + (int64_t)batch->n_seqs;
+  const int64_t units = (most < batch->n_rows ? most : batch->n_rows) * cache->n_kv_heads;
+  const int64_t deepest = few ? ceil_div(table_rows, 32) + (a.pool.bits == 8 ? kPagedStart<8> : kPagedStart<16>) : ceil_div(table_rows, 64);
+  if ((double)units * (double)deepest > (double)kPagedMostTiles || (!few && units > (1 << 24) - 1 - 2 * kPagedSlots)) {
     set_last_error("paged attention: more tiles than can be counted");
     return HI_ERR_RANGE;
   }
   StreamDevice on(stream);
-  if ((int64_t)batch->max_rows * group <= 16) return launch_paged_decode(stream, a);
-  a.positions = 128 / group;
-  // blocks of all sequences: each but the last of a sequence is full, and each has a row
-  const int64_t blocks = batch->n_rows / a.positions + batch->n_seqs;
-  const int64_t units = (blocks < batch->n_rows ? blocks : batch->n_rows) * cache->n_kv_heads;
-  return launch_paged_chunk(stream, a, units);
+  return few ? launch_paged_decode(stream, a) : launch_paged_chunk(stream, a, units);
 }

@@ -104,7 +104,7 @@ __device__ __forceinline__ uint32_t chunk_piece(const PagedAttnArgs& a, int lane
     total += over_wave(tiles * blocks, op_add);
     longest = fmaxf(longest, over_wave(tiles, op_max));
   }
-  if (!(total >= 1.f) || total > 2.1e9f) return 0;                 // (sequences that overlap could overflow the count)
+  if (!(total >= 1.f) || total > 1.01f * kPagedMostTiles) return 0;                 // (sequences that overlap could overflow the count)
   float best = longest, least = 0.f;
   const float share = total * (1.f / kPagedSlots);
 #pragma unroll

@@ -341,7 +341,7 @@ __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
     items_of_all += __builtin_amdgcn_readlane(sum_wave(mw.items), 63);
     about += over_wave((float)(mw.tiles + kStart) * (float)mw.items, op_add);
   }
-  if (about > 2.1e9f) return;
+  if (about > 1.01f * kPagedMostTiles) return;
   const uint32_t wgs = gridDim.x;
   // equal pieces: as small as a workgroup each allows, or a quarter larger
   uint32_t piece_tiles = ((uint32_t)tiles_of_all + wgs - 1) / wgs;

@@ -88,6 +88,15 @@ def test_append_far_positions():
     check(b, before, q, k, v, 10000.0, 1.0, run(b, q, k, v, 10000.0, 1.0))
 
 
+def test_append_positions_up_to_the_largest():
+    """Past lengths that end near 2^31: the queries are turned, and the rows, beyond any table, go nowhere."""
+    b = Batch([10, 5], [6, 2], page=16, kv_heads=1, group=2, width=2)
+    b.past = [(1 << 31) - 3, (1 << 31) - 1]
+    q, k, v = b.rows(2), b.rows(1), b.rows(1)
+    before = b.values()
+    check(b, before, q, k, v, 10000.0, 1.0, run(b, q, k, v, 10000.0, 1.0))
+
+
 @pytest.mark.parametrize("bits", [16, 8])
 def test_append_pages_that_are_not_there(bits):
     b = Batch([10, 30, 60], [30, 8, 12], page=16, bits=bits, seed=6, width=4)          # the last sequence runs past its table

@@ -80,6 +80,17 @@ def test_attention_past_the_end_of_the_table(hint):
 
 @pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("hint", [1, 1 << 20])
+def test_attention_of_positions_up_to_the_largest(bits, hint):
+    b = Batch([48], [3], page=16, bits=bits, seed=6, width=3)          # every row sees the whole table
+    q = b.rows(8)
+    want = attend(b, q, max_rows=hint)
+    attention_close(want, q, b.values(), b)
+    b.past = [(1 << 31) - 2]
+    assert torch.equal(attend(b, q, max_rows=hint), want)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("hint", [1, 1 << 20])
 def test_attention_of_peaked_and_of_equal_keys(bits, hint):
     b = Batch([900, 333], [1, 60], bits=bits, seed=8, kv_heads=1, group=4, page=64)
     if bits == 8:                                      # scores of up to a few hundred

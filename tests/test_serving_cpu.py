@@ -67,6 +67,7 @@ SHARED = [
     ({}, dict(row_starts=None), hb.HI_ERR_ARG), ({}, dict(page_table=A + 2), hb.HI_ERR_ARG),
     ({}, dict(n_seqs=-1), hb.HI_ERR_ARG), ({}, dict(n_rows=-1), hb.HI_ERR_ARG), ({}, dict(table_pages=0), hb.HI_ERR_ARG),
     ({}, dict(max_rows=0), hb.HI_ERR_ARG), (dict(page_rows=1024), dict(table_pages=1 << 21), hb.HI_ERR_RANGE),
+    (dict(page_rows=1024), dict(table_pages=(1 << 20) + 1), hb.HI_ERR_RANGE),
     ({}, dict(n_seqs=0, page_table=None, past_lens=None, row_starts=None), hb.HI_OK), ({}, dict(n_rows=0), hb.HI_OK)]
 
 
@@ -127,3 +128,17 @@ def test_null_structs_and_workspace_size():
 def test_struct_layouts():
     assert C.sizeof(hb.hi_paged_cache) == 32 and hb.hi_paged_cache.n_pages.offset == 16
     assert C.sizeof(hb.hi_paged_batch) == 40 and hb.hi_paged_batch.max_rows.offset == 36
+
+
+@pytest.mark.parametrize("cache,batch,kw", [
+    # (bounds from the call's own sizes, before any launch) a short table and so many sequences that the blocks' starts count
+    (dict(n_kv_heads=100), dict(n_seqs=1600000, n_rows=1600000, table_pages=1, max_rows=1), dict(n_q_heads=100)),
+    (dict(kv_bits=16, n_kv_heads=100), dict(n_seqs=3000000, n_rows=3000000, table_pages=1, max_rows=1), dict(n_q_heads=100)),
+    # a long table
+    (dict(page_rows=1024), dict(n_seqs=100, n_rows=100, table_pages=1 << 19, max_rows=1), {}),
+    (dict(page_rows=1024), dict(n_seqs=100, n_rows=1 << 20, table_pages=1 << 19, max_rows=1 << 20), {}),
+    # more blocks than a launch has workgroups
+    (dict(n_kv_heads=16), dict(n_seqs=1, n_rows=1 << 28, table_pages=1, max_rows=1 << 28), dict(n_q_heads=16)),
+    (dict(n_kv_heads=65536), {}, dict(n_q_heads=65536))])
+def test_attention_refuses_what_it_cannot_count(cache, batch, kw):
+    assert attn(cache, batch, **kw) == hb.HI_ERR_RANGE

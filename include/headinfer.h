@@ -408,8 +408,8 @@ hi_status hi_add_rmsnorm(void* stream, const void* x_dev, int32_t x_fp32, const 
  *   x_dev bf16 [n_rows][n_in], or with x_heads = 1 head-major [n_in / 128][n_rows][128] (what the attention calls write);
  *   y_dev bf16 [n_rows][n_out], or with y_heads = 1 head-major [n_out / 128][n_rows][128] (what hi_paged_append and the
  *   attention calls read: with the rows of W_Q, W_K, W_V in W, q, k and v follow each other).
- * n_in a multiple of 128, at most 2^20; n_out a multiple of 16, of 128 with y_heads (HI_ERR_UNSUPPORTED); any number of rows, n_rows = 0 does
- * nothing.  codes, x and y 16-byte aligned, scales and zeros 2-byte.
+ * n_in a multiple of 128, at most 2^20; n_out a multiple of 16, of 128 with y_heads, at most 2^24 (HI_ERR_UNSUPPORTED); any
+ * number of rows, n_rows = 0 does nothing.  codes, x and y 16-byte aligned, scales and zeros 2-byte.
  */
 hi_status hi_weight_quantize(void* stream, const void* w_dev, int32_t n_out, int32_t n_in, void* codes_dev, void* scales_dev,
                              void* zeros_dev);

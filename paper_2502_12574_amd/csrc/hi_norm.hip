@@ -48,7 +48,7 @@ template <bool XF, bool RF, int LANES, int N>
 __global__ __launch_bounds__(256) void add_rmsnorm_kernel(NormArgs a) {
   constexpr int kRows = 256 / LANES;
   const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
-  const int64_t row = (int64_t)blockIdx.x * kRows + sub;
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kRows + sub;
   const bool live = row < a.rows;
   const int64_t base = (live ? row : a.rows - 1) * a.d;
   const int pieces = a.d / 8;
@@ -116,10 +116,15 @@ __global__ __launch_bounds__(256) void add_rmsnorm_kernel(NormArgs a) {
 template <bool XF, bool RF>
 void norm_launch(hipStream_t s, const NormArgs& a) {
   const int pieces = a.d / 8;
+  // a dimension of a grid has at most 2^32 lanes
+  auto grid = [&](int rows) {
+    const int64_t n = ceil_div(a.rows, rows), x = n < (1 << 22) ? n : 1 << 22;
+    return dim3((unsigned)x, (unsigned)ceil_div(n, x));
+  };
   // rows of up to 2048 values take a wavefront each and no barrier, longer ones a workgroup
 #define HI_NORM(LANES, N)                                                                                                   \
   if (pieces <= LANES * N) {                                                                                                \
-    hipLaunchKernelGGL((add_rmsnorm_kernel<XF, RF, LANES, N>), dim3((unsigned)ceil_div(a.rows, 256 / LANES)), dim3(256), 0, s, a); \
+    hipLaunchKernelGGL((add_rmsnorm_kernel<XF, RF, LANES, N>), grid(256 / LANES), dim3(256), 0, s, a);                      \
     return;                                                                                                                 \
   }
   HI_NORM(64, 1) HI_NORM(64, 2) HI_NORM(64, 4) HI_NORM(256, 2) HI_NORM(256, 3) HI_NORM(256, 4) HI_NORM(256, 6) HI_NORM(256, 8)

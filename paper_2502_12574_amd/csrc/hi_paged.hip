@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
   static_assert(ROWS <= kAppendMostRows, "a wavefront looks each row up");
   __shared__ float2 turn[ROWS][64];
   __shared__ int place[ROWS][3];                // whether a sequence has the row, page (-1: none), row of the page
-  const int t0 = blockIdx.x * ROWS, lane = lane_id(), wave = wave_id();
+  const int t0 = (int)(blockIdx.y * gridDim.x + blockIdx.x) * ROWS, lane = lane_id(), wave = wave_id();
   const int H = a.pool.heads, heads = a.q_heads + 2 * H, tasks = heads * ROWS;
   const int c = threadIdx.x & 7;
   // task i: head i / ROWS (queries, keys, values), row i % ROWS
@@ -224,7 +224,8 @@ extern "C" hi_status hi_paged_append(void* stream, const hi_paged_cache* cache, 
     if (in_fp32) hipLaunchKernelGGL((paged_append_kernel<true, 1>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((paged_append_kernel<false, 1>), grid, dim3(256), 0, s, a);
   } else {
-    const dim3 grid((unsigned)ceil_div(batch->n_rows, 4));
+    const int64_t n = ceil_div(batch->n_rows, 4), x = n < (1 << 22) ? n : 1 << 22;      // (a dimension of a grid has at most 2^32 lanes)
+    const dim3 grid((unsigned)x, (unsigned)ceil_div(n, x));
     if (in_fp32) hipLaunchKernelGGL((paged_append_kernel<true, 4>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((paged_append_kernel<false, 4>), grid, dim3(256), 0, s, a);
   }

@@ -10,6 +10,7 @@ namespace {
 
 constexpr int kQGroup = 128;                    // input channels of a scale
 constexpr int kQMostIn = 1 << 20;               // 64 rows of x, or 16 of codes, within 32 bits of bytes
+constexpr int kQMostOut = 1 << 24;              // (a launch has at most 2^32 lanes)
 
 // ---- bf16 weights to codes: a wavefront takes 16 groups at a time, 4 lanes a group with 32 channels each.  The weights are read
 // once and a quarter of them written; run once per matrix.
@@ -447,9 +448,9 @@ int linear_form(int64_t rows, int64_t n_out, int g) {
                         1.3 + (double)ceil_div(w32, 256) * (0.5 + 0.18 * g),
                         1.5 + (double)ceil_div(w64, 256) * (1.5 + 0.30 * g),
                         (double)(t / 512) * (3 + 2.5 * g) + (rest == 0 ? 0 : rest <= 256 ? 3 + 1.33 * g : 3 + 2.4 * g)};
-  int best = 0;
-  for (int i = 1; i < 4; ++i)
-    if (us[i] < us[best]) best = i;
+  int best = 3;
+  for (int i = 0; i < 3; ++i)
+    if (us[i] < us[best] && ceil_div(rows, 16 << i) <= 65535) best = i;       // (the second dimension of a grid ends there)
   return 16 << best;
 }
 
@@ -469,7 +470,7 @@ extern "C" hi_status hi_weight_quantize(void* stream, const void* w_dev, int32_t
   if (n_out < 1 || n_in < 1) { set_last_error("weight quantise: bad shape"); return HI_ERR_ARG; }
   if (n_in % kQGroup != 0) { set_last_error("weight quantise: n_in must be a multiple of %d", kQGroup); return HI_ERR_UNSUPPORTED; }
   const int64_t groups = (int64_t)n_out * (n_in / kQGroup);
-  if (ceil_div(groups, 64) > 0x7FFFFFFF) { set_last_error("weight quantise: too many weights"); return HI_ERR_RANGE; }
+  if (ceil_div(groups, 64) >= (1 << 24)) { set_last_error("weight quantise: too many weights"); return HI_ERR_RANGE; }
   StreamDevice on(stream);
   hipLaunchKernelGGL(weight_quant_kernel, dim3((unsigned)ceil_div(groups, 64)), dim3(256), 0, (hipStream_t)stream,
                      (const uint16_t*)w_dev, groups, (char*)codes_dev, (uint16_t*)scales_dev, (uint16_t*)zeros_dev);
@@ -492,7 +493,10 @@ extern "C" hi_status hi_linear_quantized(void* stream, const void* x_dev, const 
     set_last_error("quantised linear: n_in must be a multiple of %d, n_out of 16, and of %d for head-major outputs", kQGroup, kHeadDim);
     return HI_ERR_UNSUPPORTED;
   }
-  if (n_in > kQMostIn) { set_last_error("quantised linear: n_in of more than %d", kQMostIn); return HI_ERR_UNSUPPORTED; }
+  if (n_in > kQMostIn || n_out > kQMostOut) {
+    set_last_error("quantised linear: n_in of more than %d or n_out of more than %d", kQMostIn, kQMostOut);
+    return HI_ERR_UNSUPPORTED;
+  }
   if (n_rows == 0) return HI_OK;
   StreamDevice on(stream);
   const LinearArgs a = {(const uint16_t*)x_dev, (const char*)codes_dev, (const uint16_t*)scales_dev, (const uint16_t*)zeros_dev,
@@ -507,7 +511,7 @@ extern "C" hi_status hi_linear_quantized(void* stream, const void* x_dev, const 
     case 64: e = few_turns<16, 2, 4, 2>(st, a); break;
     default: {
       const int64_t row_tiles = ceil_div(n_rows, kQTile), tiles = row_tiles * ceil_div(n_out, kQTile);
-      if (tiles > 0x7FFFFFF0) { set_last_error("quantised linear: too many rows"); return HI_ERR_RANGE; }
+      if (tiles > (1 << 24) - 8) { set_last_error("quantised linear: too many rows"); return HI_ERR_RANGE; }
       hipLaunchKernelGGL(linear_tile_kernel, dim3((unsigned)(8 * ceil_div(tiles, 8))), dim3(256), 0, st, a, (int)row_tiles);
     }
   }

@@ -121,3 +121,15 @@ def test_linear_replayed_with_new_rows():
         graph.replay()
         torch.cuda.synchronize()
         check(y, x, codes, scale, zero, k)
+
+
+def test_linear_of_more_rows_than_a_grid_dimension():
+    rows, n_in, n_out = 65535 * 16 + 40, 128, 16
+    codes, scale, zero = weights(n_out, n_in, 3)
+    x = torch.randn(rows, n_in, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).to(BF)
+    y = torch.full((rows, n_out), float("nan"), dtype=BF, device=DEV)
+    hb.hi_linear_quantized(torch.cuda.current_stream(), x, codes, scale, zero, rows, n_in, n_out, 0, 0, y)
+    torch.cuda.synchronize()
+    for at in (0, rows // 2, rows - 300):
+        check(y[at:at + 300], x[at:at + 300], codes, scale, zero, at)
+    assert torch.isfinite(y).all()

@@ -80,3 +80,15 @@ def test_norm_on_another_stream_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         check(out, res, x, r, w, 1e-5)
+
+
+def test_norm_of_more_rows_than_a_grid_dimension():
+    rows = (1 << 26) + 5                          # 4 rows to a workgroup of 256 lanes
+    x = torch.randn(rows, 8, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).to(BF)
+    w = torch.ones(8, dtype=BF, device=DEV)
+    out = torch.full_like(x, float("nan"))
+    hb.hi_add_rmsnorm(torch.cuda.current_stream(), x, 0, None, 0, w, rows, 8, 1e-5, None, out)
+    torch.cuda.synchronize()
+    for at in (0, (1 << 24) - 50, (1 << 26) - 95):
+        check(out[at:at + 100], None, x[at:at + 100], None, w, 1e-5)
+    assert torch.isfinite(out).all()

@@ -40,7 +40,7 @@ def linear(**kw):
     (dict(zeros_dev=None), hb.HI_ERR_ARG), (dict(y_dev=None), hb.HI_ERR_ARG), (dict(x_dev=OFF), hb.HI_ERR_ARG),
     (dict(codes_dev=OFF), hb.HI_ERR_ARG), (dict(scales_dev=A + 1), hb.HI_ERR_ARG), (dict(y_dev=OFF), hb.HI_ERR_ARG),
     (dict(n_rows=-1), hb.HI_ERR_ARG), (dict(n_in=0), hb.HI_ERR_ARG), (dict(n_out=-16), hb.HI_ERR_ARG),
-    (dict(n_in=(1 << 20) + 128), hb.HI_ERR_UNSUPPORTED),
+    (dict(n_in=(1 << 20) + 128), hb.HI_ERR_UNSUPPORTED), (dict(n_out=(1 << 24) + 16), hb.HI_ERR_UNSUPPORTED),
     (dict(x_heads=2), hb.HI_ERR_ARG), (dict(y_heads=-1), hb.HI_ERR_ARG), (dict(n_in=192), hb.HI_ERR_UNSUPPORTED),
     (dict(n_out=24), hb.HI_ERR_UNSUPPORTED), (dict(n_out=144, y_heads=1), hb.HI_ERR_UNSUPPORTED), (dict(n_rows=0), hb.HI_OK)])
 def test_linear_refusals(kw, status):

@@ -380,7 +380,8 @@ hi_status hi_kv_dequantize(void* stream, const void* packed_dev, int64_t n_rows,
 
 /*
  * Serving a batch of sequences from one pool of cache pages (Section 3.2 notes that the head-wise partition extends to the
- * batch dimension; the contexts above serve one sequence each).  All of it stateless: device buffers and a stream.  A layer's
+ * batch dimension; the contexts above serve one sequence each).  All of it stateless: device buffers and a stream (of any device;
+ * null is the null stream of the current one), and with no rows null buffers will do.  A layer's
  * step over the new rows of all sequences, back to back in [rows]-first buffers, is
  *   hi_add_rmsnorm -> hi_qkv_rope (rope_theta = 0) or hi_linear_quantized -> hi_paged_append -> hi_paged_attn
  *   -> hi_out_proj or hi_linear_quantized -> the next hi_add_rmsnorm.
@@ -390,7 +391,8 @@ hi_status hi_kv_dequantize(void* stream, const void* packed_dev, int64_t n_rows,
  *   x_dev [n_rows][d], bf16 or fp32 (x_fp32); residual_dev the same shape, bf16 or fp32 (residual_fp32), or null: h = x;
  *   weight_dev bf16 [d]; residual_out_dev in the residual's type, or null: not written; out_dev bf16 [n_rows][d].
  *   residual_out_dev may be residual_dev (in place) and out_dev may be a bf16 x_dev; other overlaps are not allowed.  d a
- *   multiple of 8, at most 16384 (HI_ERR_UNSUPPORTED); eps >= 0; n_rows = 0 does nothing.
+ *   multiple of 8, at most 16384 (HI_ERR_UNSUPPORTED); eps >= 0; n_rows = 0 does nothing.  (A sum of squares beyond fp32 is
+ *   infinite, and out is zeros.)
  */
 hi_status hi_add_rmsnorm(void* stream, const void* x_dev, int32_t x_fp32, const void* residual_dev, int32_t residual_fp32,
                          const void* weight_dev, int32_t n_rows, int32_t d, float eps, void* residual_out_dev, void* out_dev);
@@ -463,7 +465,7 @@ typedef struct hi_paged_batch {
  *   2^-100 is stored as zeros with scale 0).
  * hi_paged_attn: out[j][t][:] = softmax_i(q[j][t] . K[i] / sqrt(128)) V[i] over the cached rows i = 0 .. position of t of t's
  *   sequence, for query head j and KV head j / (n_q_heads / n_kv_heads); call hi_paged_append first, the step's own rows are
- *   read from the pages too.  q_dev and out_dev bf16 [n_q_heads][n_rows][128]; q_prescaled as in hi_problem.  Scores, maxima,
+ *   read from the pages too.  q_dev and out_dev bf16 [n_q_heads][n_rows][128], apart from each other; q_prescaled as in hi_problem.  Scores, maxima,
  *   sums and outputs are held in fp32; weights are rounded to bf16 for the second product.  1 to 16 query heads a KV head.
  *   workspace_dev: DEVICE, hi_paged_workspace_bytes bytes, filled with zeros once before its first use; a call leaves it fit
  *   for the next one.  Calls that may overlap in time need workspaces of their own, as do captured graphs that may.

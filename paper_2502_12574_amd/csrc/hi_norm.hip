@@ -140,7 +140,6 @@ using namespace hi;
 extern "C" hi_status hi_add_rmsnorm(void* stream, const void* x_dev, int32_t x_fp32, const void* residual_dev,
                                     int32_t residual_fp32, const void* weight_dev, int32_t n_rows, int32_t d, float eps,
                                     void* residual_out_dev, void* out_dev) {
-  if (!x_dev || !weight_dev || !out_dev) { set_last_error("norm: null buffer"); return HI_ERR_ARG; }
   if (!aligned_to(x_dev, 16) || !aligned_to(residual_dev, 16) || !aligned_to(weight_dev, 16) || !aligned_to(residual_out_dev, 16) ||
       !aligned_to(out_dev, 16)) {
     set_last_error("norm: buffers must be 16-byte aligned");
@@ -154,8 +153,10 @@ extern "C" hi_status hi_add_rmsnorm(void* stream, const void* x_dev, int32_t x_f
     set_last_error("norm: rows must be a multiple of 8 values and at most %d long", kNormMaxD);
     return HI_ERR_UNSUPPORTED;
   }
+  if (n_rows == 0) return HI_OK;                 // (whose buffers may be null)
+  if (!x_dev || !weight_dev || !out_dev) { set_last_error("norm: null buffer"); return HI_ERR_ARG; }
   if (x_fp32 && x_dev == out_dev) { set_last_error("norm: an fp32 x cannot be the bf16 output"); return HI_ERR_ARG; }
-  if (n_rows == 0) return HI_OK;
+  if (out_dev == residual_dev || out_dev == residual_out_dev) { set_last_error("norm: the output cannot be the residual"); return HI_ERR_ARG; }
   StreamDevice on(stream);
   const NormArgs a = {x_dev, residual_dev, (const uint16_t*)weight_dev, residual_out_dev, (uint16_t*)out_dev, n_rows, d, eps};
   const hipStream_t s = (hipStream_t)stream;

@@ -198,18 +198,18 @@ extern "C" hi_status hi_paged_append(void* stream, const hi_paged_cache* cache, 
   AppendArgs a = {};
   const hi_status st = paged_arguments(cache, batch, "append", a.pool, a.seqs);
   if (st != HI_OK) return st;
-  if (!k_in_dev || !v_in_dev || !q_in_dev != !q_out_dev) { set_last_error("append: null buffer"); return HI_ERR_ARG; }
   if (!aligned_to(q_in_dev, 16) || !aligned_to(k_in_dev, 16) || !aligned_to(v_in_dev, 16) || !aligned_to(q_out_dev, 16)) {
     set_last_error("append: buffers must be 16-byte aligned");
     return HI_ERR_ARG;
   }
-  if ((in_fp32 != 0 && in_fp32 != 1) || n_q_heads < (q_in_dev ? 1 : 0) || n_q_heads > (1 << 20) || cache->n_kv_heads > (1 << 20) ||
+  if ((in_fp32 != 0 && in_fp32 != 1) || n_q_heads < (q_in_dev || q_out_dev ? 1 : 0) || n_q_heads > (1 << 20) || cache->n_kv_heads > (1 << 20) ||
       !(rope_theta >= 0) || !(rope_theta < 1e300) || !(q_scale > 0.0f) || !(q_scale < 3.0e38f)) {
     set_last_error("append: bad shape, rope_theta or q_scale");
     return HI_ERR_ARG;
   }
+  if (batch->n_seqs == 0 || batch->n_rows == 0) return HI_OK;      // (whose buffers may be null)
+  if (!k_in_dev || !v_in_dev || !q_in_dev != !q_out_dev) { set_last_error("append: null buffer"); return HI_ERR_ARG; }
   if (in_fp32 && q_in_dev && q_in_dev == q_out_dev) { set_last_error("append: fp32 queries cannot be rotated in place"); return HI_ERR_ARG; }
-  if (batch->n_seqs == 0 || batch->n_rows == 0) return HI_OK;
   a.q = q_in_dev; a.k = k_in_dev; a.v = v_in_dev; a.q_out = (uint16_t*)q_out_dev;
   a.q_heads = q_in_dev ? n_q_heads : 0;
   a.q_scale = q_scale;

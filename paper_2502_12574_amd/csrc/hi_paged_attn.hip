@@ -27,7 +27,6 @@ extern "C" hi_status hi_paged_attn(void* stream, const hi_paged_cache* cache, co
   PagedAttnArgs a = {};
   const hi_status st = paged_arguments(cache, batch, "paged attention", a.pool, a.seqs);
   if (st != HI_OK) return st;
-  if (!q_dev || !out_dev || !workspace_dev) { set_last_error("paged attention: null buffer"); return HI_ERR_ARG; }
   if (!aligned_to(q_dev, 16) || !aligned_to(out_dev, 16) || !aligned_to(workspace_dev, 16)) {
     set_last_error("paged attention: buffers must be 16-byte aligned");
     return HI_ERR_ARG;
@@ -37,7 +36,9 @@ extern "C" hi_status hi_paged_attn(void* stream, const hi_paged_cache* cache, co
   if (group > 16) { set_last_error("paged attention: at most 16 query heads a KV head"); return HI_ERR_UNSUPPORTED; }
   // (the scales of all heads of a page lie within 32 bits of bytes)
   if (n_q_heads > 65535) { set_last_error("paged attention: too many heads"); return HI_ERR_RANGE; }
-  if (batch->n_seqs == 0 || batch->n_rows == 0) return HI_OK;
+  if (batch->n_seqs == 0 || batch->n_rows == 0) return HI_OK;      // (whose buffers may be null)
+  if (!q_dev || !out_dev || !workspace_dev) { set_last_error("paged attention: null buffer"); return HI_ERR_ARG; }
+  if (q_dev == out_dev) { set_last_error("paged attention: the output cannot be the queries"); return HI_ERR_ARG; }
   a.q = (const uint16_t*)q_dev; a.out = (uint16_t*)out_dev;
   a.group = group;
   a.c = softmax_scale_log2(q_prescaled != 0);

@@ -480,7 +480,6 @@ extern "C" hi_status hi_weight_quantize(void* stream, const void* w_dev, int32_t
 extern "C" hi_status hi_linear_quantized(void* stream, const void* x_dev, const void* codes_dev, const void* scales_dev,
                                          const void* zeros_dev, int32_t n_rows, int32_t n_in, int32_t n_out, int32_t x_heads,
                                          int32_t y_heads, void* y_dev) {
-  if (!x_dev || !codes_dev || !scales_dev || !zeros_dev || !y_dev) { set_last_error("quantised linear: null buffer"); return HI_ERR_ARG; }
   if (!aligned_to(x_dev, 16) || !aligned_to(codes_dev, 16) || !aligned_to(scales_dev, 2) || !aligned_to(zeros_dev, 2) || !aligned_to(y_dev, 16)) {
     set_last_error("quantised linear: rows and codes must be 16-byte aligned, scales and zeros 2-byte");
     return HI_ERR_ARG;
@@ -497,7 +496,9 @@ extern "C" hi_status hi_linear_quantized(void* stream, const void* x_dev, const 
     set_last_error("quantised linear: n_in of more than %d or n_out of more than %d", kQMostIn, kQMostOut);
     return HI_ERR_UNSUPPORTED;
   }
-  if (n_rows == 0) return HI_OK;
+  if (n_rows == 0) return HI_OK;                 // (whose buffers may be null)
+  if (!x_dev || !codes_dev || !scales_dev || !zeros_dev || !y_dev) { set_last_error("quantised linear: null buffer"); return HI_ERR_ARG; }
+  if (y_dev == x_dev) { set_last_error("quantised linear: y cannot be x"); return HI_ERR_ARG; }
   StreamDevice on(stream);
   const LinearArgs a = {(const uint16_t*)x_dev, (const char*)codes_dev, (const uint16_t*)scales_dev, (const uint16_t*)zeros_dev,
                         (uint16_t*)y_dev, n_rows, n_in, n_out, x_heads, y_heads};

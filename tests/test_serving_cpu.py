@@ -7,11 +7,12 @@ from paper_2502_12574_amd import binding as hb
 
 A = 0x10000                                    # an aligned address that nobody follows
 OFF = A + 8
+B = A + 0x10000
 
 
 def norm(**kw):
     a = dict(stream=None, x_dev=A, x_fp32=0, residual_dev=A, residual_fp32=0, weight_dev=A, n_rows=4, d=64, eps=1e-5,
-             residual_out_dev=A, out_dev=A)
+             residual_out_dev=A, out_dev=B)
     a.update(kw)
     return hb.hi_add_rmsnorm(**a, check=False)
 
@@ -22,15 +23,17 @@ def norm(**kw):
     (dict(weight_dev=OFF), hb.HI_ERR_ARG), (dict(out_dev=OFF), hb.HI_ERR_ARG), (dict(n_rows=-1), hb.HI_ERR_ARG),
     (dict(d=0), hb.HI_ERR_ARG), (dict(x_fp32=2), hb.HI_ERR_ARG), (dict(residual_fp32=-1), hb.HI_ERR_ARG),
     (dict(eps=-1.0), hb.HI_ERR_ARG), (dict(eps=float("nan")), hb.HI_ERR_ARG), (dict(eps=float("inf")), hb.HI_ERR_ARG),
-    (dict(x_fp32=1), hb.HI_ERR_ARG),                                      # an fp32 x and a bf16 output in one buffer
-    (dict(d=60), hb.HI_ERR_UNSUPPORTED), (dict(d=16392), hb.HI_ERR_UNSUPPORTED), (dict(n_rows=0), hb.HI_OK)])
+    (dict(x_fp32=1, out_dev=A, residual_dev=None, residual_out_dev=None), hb.HI_ERR_ARG),                                # an fp32 x and a bf16 output in one buffer
+    (dict(d=60), hb.HI_ERR_UNSUPPORTED), (dict(d=16392), hb.HI_ERR_UNSUPPORTED), (dict(n_rows=0), hb.HI_OK),
+    (dict(out_dev=A), hb.HI_ERR_ARG), (dict(out_dev=A, residual_out_dev=B), hb.HI_ERR_ARG),              # the residual's buffers
+    (dict(n_rows=0, x_dev=None, residual_dev=None, residual_out_dev=None, out_dev=None), hb.HI_OK)])
 def test_norm_refusals(kw, status):
     assert norm(**kw) == status
 
 
 def linear(**kw):
     a = dict(stream=None, x_dev=A, codes_dev=A, scales_dev=A, zeros_dev=A, n_rows=3, n_in=256, n_out=128, x_heads=0, y_heads=0,
-             y_dev=A)
+             y_dev=B)
     a.update(kw)
     return hb.hi_linear_quantized(**a, check=False)
 
@@ -42,7 +45,8 @@ def linear(**kw):
     (dict(n_rows=-1), hb.HI_ERR_ARG), (dict(n_in=0), hb.HI_ERR_ARG), (dict(n_out=-16), hb.HI_ERR_ARG),
     (dict(n_in=(1 << 20) + 128), hb.HI_ERR_UNSUPPORTED), (dict(n_out=(1 << 24) + 16), hb.HI_ERR_UNSUPPORTED),
     (dict(x_heads=2), hb.HI_ERR_ARG), (dict(y_heads=-1), hb.HI_ERR_ARG), (dict(n_in=192), hb.HI_ERR_UNSUPPORTED),
-    (dict(n_out=24), hb.HI_ERR_UNSUPPORTED), (dict(n_out=144, y_heads=1), hb.HI_ERR_UNSUPPORTED), (dict(n_rows=0), hb.HI_OK)])
+    (dict(n_out=24), hb.HI_ERR_UNSUPPORTED), (dict(n_out=144, y_heads=1), hb.HI_ERR_UNSUPPORTED), (dict(n_rows=0), hb.HI_OK),
+    (dict(y_dev=A), hb.HI_ERR_ARG), (dict(n_rows=0, x_dev=None, y_dev=None), hb.HI_OK)])
 def test_linear_refusals(kw, status):
     assert linear(**kw) == status
 
@@ -82,7 +86,7 @@ def append(cache={}, batch={}, **kw):
 
 
 def attn(cache={}, batch={}, **kw):
-    a = dict(q_dev=A, n_q_heads=4, q_prescaled=0, out_dev=A, workspace_dev=A)
+    a = dict(q_dev=A, n_q_heads=4, q_prescaled=0, out_dev=B, workspace_dev=A)
     a.update(kw)
     return hb.hi_paged_attn(None, *structs(cache, batch), **a, check=False)
 
@@ -99,7 +103,7 @@ def test_paged_cache_and_batch_refusals(cache, batch, status):
     (dict(in_fp32=3), hb.HI_ERR_ARG), (dict(n_q_heads=0), hb.HI_ERR_ARG), (dict(rope_theta=-1.0), hb.HI_ERR_ARG),
     (dict(rope_theta=float("nan")), hb.HI_ERR_ARG), (dict(rope_theta=float("inf")), hb.HI_ERR_ARG),
     (dict(q_scale=0.0), hb.HI_ERR_ARG), (dict(q_scale=float("nan")), hb.HI_ERR_ARG),
-    (dict(in_fp32=1), hb.HI_ERR_ARG)])                                     # fp32 queries in place of bf16 ones
+    (dict(n_q_heads=0, q_in_dev=None), hb.HI_ERR_ARG), (dict(in_fp32=1), hb.HI_ERR_ARG)])    # fp32 queries in place of bf16 ones
 def test_append_refusals(kw, status):
     assert append(**kw) == status
 
@@ -107,7 +111,8 @@ def test_append_refusals(kw, status):
 @pytest.mark.parametrize("kw,status", [
     (dict(q_dev=None), hb.HI_ERR_ARG), (dict(out_dev=None), hb.HI_ERR_ARG), (dict(workspace_dev=None), hb.HI_ERR_ARG),
     (dict(q_dev=OFF), hb.HI_ERR_ARG), (dict(workspace_dev=OFF), hb.HI_ERR_ARG), (dict(n_q_heads=3), hb.HI_ERR_ARG),
-    (dict(n_q_heads=0), hb.HI_ERR_ARG), (dict(q_prescaled=2), hb.HI_ERR_ARG), (dict(n_q_heads=34), hb.HI_ERR_UNSUPPORTED)])
+    (dict(n_q_heads=0), hb.HI_ERR_ARG), (dict(q_prescaled=2), hb.HI_ERR_ARG), (dict(n_q_heads=34), hb.HI_ERR_UNSUPPORTED),
+    (dict(out_dev=A), hb.HI_ERR_ARG)])
 def test_attention_refusals(kw, status):
     assert attn(**kw) == status
 
@@ -142,3 +147,9 @@ def test_struct_layouts():
     (dict(n_kv_heads=65536), {}, dict(n_q_heads=65536))])
 def test_attention_refuses_what_it_cannot_count(cache, batch, kw):
     assert attn(cache, batch, **kw) == hb.HI_ERR_RANGE
+
+
+def test_a_step_without_rows_needs_no_buffers():
+    for batch in (dict(n_rows=0), dict(n_seqs=0)):
+        assert append({}, batch, q_in_dev=None, k_in_dev=None, v_in_dev=None, q_out_dev=None) == hb.HI_OK
+        assert attn({}, batch, q_dev=None, out_dev=None) == hb.HI_OK

@@ -103,7 +103,7 @@ def _load_native():
                                                          L.hi_qkv_rope, L.hi_out_proj)], C.c_void_p)
     serving = [getattr(L, name, None) for name in ("hi_add_rmsnorm", "hi_linear_quantized", "hi_paged_append", "hi_paged_attn")]
     if None not in serving:
-        _pycall.bind_serving(*[C.cast(f, C.c_void_p).value for f in serving])
+        _pycall.bind_serving(*[C.cast(f, C.c_void_p).value for f in serving], hi_paged_cache, hi_paged_batch)
     _native = _pycall
     return _native
 
@@ -385,7 +385,6 @@ def make_paged_cache(pages, scales, n_pages, n_kv_heads, page_rows, kv_bits=16) 
     """pages: [n_pages][n_kv_heads][2][page_rows][128] bf16 (kv_bits 16) or e4m3 (8); scales: fp32 without the last axis, or None."""
     c = hi_paged_cache(_ptr(pages), _ptr(scales), n_pages, n_kv_heads, page_rows, kv_bits)
     c._keepalive = (pages, scales)                    # the struct only holds addresses
-    c.address = C.addressof(c)                        # (its own, for the native marshalling)
     return c
 
 
@@ -393,7 +392,6 @@ def make_paged_batch(page_table, past_lens, row_starts, n_seqs, table_pages, n_r
     """page_table [n_seqs][table_pages], past_lens [n_seqs], row_starts [n_seqs + 1]: int32 on the device."""
     b = hi_paged_batch(_ptr(page_table), _ptr(past_lens), _ptr(row_starts), n_seqs, table_pages, n_rows, max_rows)
     b._keepalive = (page_table, past_lens, row_starts)
-    b.address = C.addressof(b)
     return b
 
 

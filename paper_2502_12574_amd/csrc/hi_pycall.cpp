@@ -20,7 +20,7 @@ decltype(&hi_add_rmsnorm) f_norm;
 decltype(&hi_linear_quantized) f_linear;
 decltype(&hi_paged_append) f_append;
 decltype(&hi_paged_attn) f_attn;
-PyObject *s_data_ptr, *s_cuda_stream, *s_value, *s_address, *c_void_p_type;
+PyObject *s_data_ptr, *s_cuda_stream, *s_value, *c_void_p_type, *cache_type, *batch_type;
 
 // One call's arguments.  ok goes down at the first unusual one; a Python error (of a data_ptr, say) is kept and raised.
 struct Args {
@@ -62,11 +62,14 @@ struct Args {
     return from(PyObject_GetAttr(a[i], s_cuda_stream));
   }
   template <class T>
-  const T* structure(Py_ssize_t i) {              // a ctypes structure that knows its own address
-    if (!ok || a[i] == Py_None || PyLong_Check(a[i])) { ok = false; return nullptr; }
-    PyObject* const got = PyObject_GetAttr(a[i], s_address);
-    if (!got) { PyErr_Clear(); ok = false; return nullptr; }
-    return (const T*)from(got);
+  const T* structure(Py_ssize_t i, PyObject* type) {      // a ctypes structure of that type: its buffer is the structure itself
+    if (!ok || (PyObject*)Py_TYPE(a[i]) != type) { ok = false; return nullptr; }
+    Py_buffer view;
+    if (PyObject_GetBuffer(a[i], &view, PyBUF_SIMPLE) != 0) { PyErr_Clear(); ok = false; return nullptr; }
+    const T* const at = (const T*)view.buf;
+    ok = view.len == (Py_ssize_t)sizeof(T);
+    PyBuffer_Release(&view);                      // (the caller holds the structure for as long as the call takes)
+    return at;
   }
   hi_ctx* context(Py_ssize_t i) {
     if (!ok || a[i] == Py_None || PyLong_Check(a[i])) return ok ? (hi_ctx*)address(a[i]) : nullptr;
@@ -182,8 +185,8 @@ PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!f_append || n != 11) Py_RETURN_NONE;
   Args g{a};
   void* s = g.stream(0);
-  const hi_paged_cache* c = g.structure<hi_paged_cache>(1);
-  const hi_paged_batch* b = g.structure<hi_paged_batch>(2);
+  const hi_paged_cache* c = g.structure<hi_paged_cache>(1, cache_type);
+  const hi_paged_batch* b = g.structure<hi_paged_batch>(2, batch_type);
   void *q = g.buffer(3), *k = g.buffer(4), *v = g.buffer(5);
   const int32_t fp32 = g.int32(6), heads = g.int32(7);
   const double theta = g.real(8);
@@ -196,17 +199,18 @@ PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!f_attn || n != 8) Py_RETURN_NONE;
   Args g{a};
   void* s = g.stream(0);
-  const hi_paged_cache* c = g.structure<hi_paged_cache>(1);
-  const hi_paged_batch* b = g.structure<hi_paged_batch>(2);
+  const hi_paged_cache* c = g.structure<hi_paged_cache>(1, cache_type);
+  const hi_paged_batch* b = g.structure<hi_paged_batch>(2, batch_type);
   void* q = g.buffer(3);
   const int32_t heads = g.int32(4), pre = g.int32(5);
   void *out = g.buffer(6), *ws = g.buffer(7);
   return run(g, [&] { return f_attn(s, c, b, q, heads, pre, out, ws); });
 }
 
-// bind_serving(add_rmsnorm, linear_quantized, paged_append, paged_attn): the functions' addresses
+// bind_serving(add_rmsnorm, linear_quantized, paged_append, paged_attn, hi_paged_cache, hi_paged_batch): the functions' addresses, and
+// the types of the structures
 PyObject* bind_serving(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 4) { PyErr_SetString(PyExc_TypeError, "bind_serving takes four addresses"); return nullptr; }
+  if (n != 6) { PyErr_SetString(PyExc_TypeError, "bind_serving takes four addresses and two types"); return nullptr; }
   void* p[4];
   for (int i = 0; i < 4; ++i) {
     p[i] = PyLong_AsVoidPtr(a[i]);
@@ -216,6 +220,10 @@ PyObject* bind_serving(PyObject*, PyObject* const* a, Py_ssize_t n) {
   f_linear = (decltype(f_linear))p[1];
   f_append = (decltype(f_append))p[2];
   f_attn = (decltype(f_attn))p[3];
+  Py_XDECREF(cache_type);
+  Py_XDECREF(batch_type);
+  Py_INCREF(cache_type = a[4]);
+  Py_INCREF(batch_type = a[5]);
   Py_RETURN_NONE;
 }
 
@@ -258,7 +266,6 @@ PyMODINIT_FUNC PyInit__pycall(void) {
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
   s_value = PyUnicode_InternFromString("value");
-  s_address = PyUnicode_InternFromString("address");
-  if (!s_data_ptr || !s_cuda_stream || !s_value || !s_address) return nullptr;
+  if (!s_data_ptr || !s_cuda_stream || !s_value) return nullptr;
   return PyModule_Create(&module_def);
 }

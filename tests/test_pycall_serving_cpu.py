@@ -49,11 +49,11 @@ ORDINARY = [
     lambda: hb.hi_linear_quantized(None, T, T, T[8:], T, 3, 256, 128, 1, 0, T, check=False),
     lambda: hb.hi_paged_append(_Stream(), CACHE, BATCH, None, T, T[8:], 1, 0, 5e5, 0.125, None, check=False),
     lambda: hb.hi_paged_attn(0x7F0000001000, CACHE, BATCH, T, 8, 1, T, T[8:], check=False),
+    lambda: hb.hi_paged_append(None, hb.hi_paged_cache(1, 2, 3, 4, 5, 6), hb.hi_paged_batch.from_buffer_copy(BATCH), None, T, T, 1, 0, 5e5, 0.125, None, check=False),
 ]
 UNUSUAL = [
     lambda: hb.hi_add_rmsnorm(_Stream(), T, 0, T, 1, T, 3, 64, 1, None, T, check=False),                    # an int for a float
     lambda: hb.hi_paged_attn(None, C.byref(CACHE), BATCH, T, 8, 1, T, T, check=False),                      # a structure by reference
-    lambda: hb.hi_paged_append(None, hb.hi_paged_cache(1, 2, 3, 4, 5, 6), BATCH, None, T, T, 1, 0, 5e5, 0.125, None, check=False),
 ]
 
 
@@ -77,3 +77,18 @@ def test_native_and_ctypes_agree(seen, monkeypatch, i):
     monkeypatch.setattr(hb, "_native", hb._CtypesOnly)
     assert call() == -5
     assert first == seen.pop() and not seen
+
+
+def test_a_copied_structure_is_its_own(seen):
+    """What a copy holds counts, not what it was copied from."""
+    batch = hb.hi_paged_batch.from_buffer_copy(BATCH)
+    batch.n_rows = 99
+    hb.hi_paged_attn(None, CACHE, batch, T, 8, 1, T, T, check=False)
+    assert seen.pop()[1][2][5] == 99
+
+
+def test_structures_in_the_wrong_place_are_refused(seen):
+    for cache, batch in ((BATCH, CACHE), (CACHE, CACHE), (CACHE, bytes(40)), (None, 3.0)):
+        with pytest.raises(C.ArgumentError):
+            hb.hi_paged_attn(None, cache, batch, T, 8, 1, T, T, check=False)
+    assert not seen

@@ -13,16 +13,23 @@ import torch
 from . import binding as hb
 
 
-class QuantizedWeight:
-    """A weight matrix [n_out][n_in] in 4 bits (hi_weight_quantize): codes, and a scale and a zero for each 128 of a row."""
+def _check_buffer(what, t, dtypes, device):
+    dtypes = dtypes if isinstance(dtypes, tuple) else (dtypes,)
+    if t.dtype not in dtypes or t.device != device or not t.is_contiguous():
+        raise RuntimeError(f"{what}: {t.dtype} of strides {t.stride()} on {t.device}; wanted are contiguous rows of {dtypes} on {device}")
 
-    def __init__(self, w: torch.Tensor, stream=None):
-        assert w.dtype == torch.bfloat16 and w.is_contiguous() and w.dim() == 2
+
+class QuantizedWeight:
+    """A weight matrix [n_out][n_in] in 4 bits (hi_weight_quantize): codes, and a scale and a zero for each 128 of a row.  Made on the
+    current stream."""
+
+    def __init__(self, w: torch.Tensor):
+        _check_buffer("weight", w, torch.bfloat16, w.device)
         self.n_out, self.n_in = w.shape
         self.codes = torch.empty(self.n_out, self.n_in // 2, dtype=torch.uint8, device=w.device)
         self.scales, self.zeros = (torch.empty(self.n_out, self.n_in // 128, dtype=torch.bfloat16, device=w.device) for _ in range(2))
         with torch.cuda.device(w.device):
-            hb.hi_weight_quantize(stream or torch.cuda.current_stream(), w, self.n_out, self.n_in, self.codes, self.scales, self.zeros)
+            hb.hi_weight_quantize(torch.cuda.current_stream(), w, self.n_out, self.n_in, self.codes, self.scales, self.zeros)
 
     @property
     def shape(self):
@@ -37,6 +44,8 @@ class PagePool:
 
     def __init__(self, n_layers, n_kv_heads, n_pages, page_rows=64, kv_bits=16, max_seqs=64, max_context=1 << 17, device="cuda:0"):
         self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
         self.n_pages, self.page_rows, self.n_kv_heads = n_pages, page_rows, n_kv_heads
         shape = (n_pages, n_kv_heads, 2, page_rows, 128)
         dt = torch.bfloat16 if kv_bits == 16 else torch.float8_e4m3fn
@@ -56,8 +65,11 @@ class PagePool:
         self.length[slot] = 0
         return slot
 
+    def _open(self, slot) -> bool:
+        return 0 <= slot < len(self.owned) and slot not in self.idle
+
     def close(self, slot: int):
-        if slot in self.idle:
+        if not self._open(slot):
             raise RuntimeError(f"slot {slot} is not open")
         self.free += reversed(self.owned[slot])
         self.owned[slot] = []
@@ -68,7 +80,7 @@ class PagePool:
         if there are more than that.  The sequences count as that much longer from here on."""
         slots, new_rows = list(slots), list(new_rows)
         total = sum(new_rows)
-        if len(set(slots)) != len(slots) or any(s in self.idle for s in slots) or any(n < 0 for n in new_rows) or len(slots) != len(new_rows):
+        if len(set(slots)) != len(slots) or not all(map(self._open, slots)) or any(n < 0 for n in new_rows) or len(slots) != len(new_rows):
             raise RuntimeError("a step takes open slots, each once, and a number of rows for each")
         if n_rows is not None and n_rows < total:
             raise RuntimeError(f"{total} new rows in buffers of {n_rows}")
@@ -106,23 +118,36 @@ class PagedBlock:
         self.Hq = w_o.shape[1] // 128
         assert w_qkv.shape == ((self.Hq + 2 * self.Hkv) * 128, self.D) and w_o.shape[1] == self.Hq * 128 and norm_weight.shape == (self.D,)
         dev, heads = pool.device, self.Hq + 2 * self.Hkv
+        for what, w in (("norm weight", norm_weight), ("w_qkv", w_qkv), ("w_o", w_o)):
+            if not isinstance(w, QuantizedWeight):
+                _check_buffer(what, w, torch.bfloat16, dev)
         self.stream = stream or torch.cuda.current_stream(dev)
         # a bf16 projection hands over its fp32 sums, so that queries, keys and values are rounded once, behind the rotation
         self.fp32 = not isinstance(w_qkv, QuantizedWeight)
-        self.qkv = torch.empty(heads * max_rows * 128, dtype=torch.float32 if self.fp32 else torch.bfloat16, device=dev)
-        self.q = torch.empty(self.Hq * max_rows * 128, dtype=torch.bfloat16, device=dev)
-        self.attn = torch.empty(self.Hq * max_rows * 128, dtype=torch.bfloat16, device=dev)
-        self.h = torch.empty(max_rows, self.D, dtype=torch.bfloat16, device=dev)
-        self.workspace = torch.zeros(hb.hi_paged_workspace_bytes(self.Hq, self.Hkv), dtype=torch.uint8, device=dev)
-        torch.cuda.current_stream(dev).synchronize()         # (filled, before another stream uses it)
+        torch.cuda.current_stream(dev).synchronize()         # (the pool and the weights, before another stream uses them)
+        with torch.cuda.stream(self.stream):                 # the block's own buffers belong to its stream
+            self.qkv = torch.empty(heads * max_rows * 128, dtype=torch.float32 if self.fp32 else torch.bfloat16, device=dev)
+            self.q = torch.empty(self.Hq * max_rows * 128, dtype=torch.bfloat16, device=dev)
+            self.attn = torch.empty(self.Hq * max_rows * 128, dtype=torch.bfloat16, device=dev)
+            self.h = torch.empty(max_rows, self.D, dtype=torch.bfloat16, device=dev)
+            self.workspace = torch.zeros(hb.hi_paged_workspace_bytes(self.Hq, self.Hkv), dtype=torch.uint8, device=dev)
 
     def forward(self, x: torch.Tensor, residual, batch: hb.hi_paged_batch, y: torch.Tensor):
         """x bf16 [n][d_model], n = batch.n_rows: what the block before put out; residual bf16 or fp32 [n][d_model], to which x is added
-        in place, or None; y bf16 [n][d_model] receives the block's output.  Enqueues on the block's stream."""
-        n = batch.n_rows
-        if x.shape != (n, self.D) or y.shape != (n, self.D) or n > self.max_rows:
-            raise RuntimeError(f"rows of {tuple(x.shape)} and {tuple(y.shape)} for a batch of {n}: the block takes [n][{self.D}], at most {self.max_rows}")
+        in place, or None; y bf16 [n][d_model] receives the block's output.  Enqueues on the block's stream, which the caller orders
+        behind whatever makes x and residual; the tensors, and the batch, may be let go of when this returns."""
+        n, dev = batch.n_rows, self.pool.device
+        for t in (x, y) if residual is None else (x, y, residual):
+            if t.shape != (n, self.D) or n > self.max_rows:
+                raise RuntimeError(f"rows of {tuple(t.shape)} for a batch of {n}: the block takes [n][{self.D}], at most {self.max_rows}")
+            _check_buffer("rows", t, (torch.bfloat16, torch.float32) if t is residual else torch.bfloat16, dev)
+        if n == 0:
+            return y
         s, cache = self.stream, self.pool.caches[self.layer]
+        if s != torch.cuda.current_stream(dev):              # (where their memory would be given out again)
+            for t in (x, y, residual, *batch._keepalive):
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(s)
         # a launch goes to a stream of the current device
         with torch.cuda.device(self.pool.device):
             hb.hi_add_rmsnorm(s, x, 0, residual, int(residual is not None and residual.dtype == torch.float32), self.norm_weight, n, self.D,

@@ -157,3 +157,49 @@ def test_block_refuses_rows_that_do_not_fit():
         block.forward(x, None, batch, x)
     with pytest.raises(RuntimeError):
         block.forward(x[:4], None, batch, x[:4])
+
+
+def test_block_refuses_rows_of_other_layouts_and_takes_none():
+    w_qkv, w_o, norm = weights(44)
+    pool = PagePool(1, HKV, 8, page_rows=16, max_seqs=1, max_context=64, device=DEV)
+    block = PagedBlock(pool, 0, norm, w_qkv, w_o, 8, THETA)
+    slot = pool.open()
+    batch = pool.step([slot], [4])
+    x, wide = torch.zeros(4, D, dtype=BF, device=DEV), torch.zeros(4, 2 * D, dtype=BF, device=DEV)
+    for args in ((wide[:, :D], None, x), (x, None, wide[:, :D]), (x, wide[:, :D], x), (x, x[:2], x), (x.float(), None, x),
+                 (x, x.to(torch.float16), x), (x.cpu(), None, x), (x, None, x.float())):
+        with pytest.raises(RuntimeError):
+            block.forward(*args[:2], batch, args[2])
+    with pytest.raises(RuntimeError):
+        PagedBlock(pool, 0, norm, w_qkv.t().contiguous().t(), w_o, 8, THETA)
+    with pytest.raises(RuntimeError):
+        QuantizedWeight(w_o.float())
+    none = x[:0]
+    assert block.forward(none, None, pool.step([], []), none) is none
+
+
+def test_a_block_on_a_stream_of_its_own_while_memory_is_given_out_again():
+    """Batches and rows are let go of at once: what the current stream allocates and fills next must not be theirs while the block runs."""
+    w_qkv, w_o, norm = weights(45)
+    g = torch.Generator().manual_seed(5)
+    rows = [torch.randn(n, D, generator=g).to(BF) for n in (300, 40, 40, 40)]
+    outs = []
+    for own in (False, True):
+        pool = PagePool(1, HKV, 60, page_rows=16, max_seqs=1, max_context=960, device=DEV)
+        stream = torch.cuda.Stream() if own else None
+        block, slot, ys = PagedBlock(pool, 0, norm, w_qkv, w_o, 300, THETA, stream=stream), pool.open(), []
+        for x in rows:
+            x = x.to(DEV)
+            y = torch.empty_like(x)
+            torch.cuda.current_stream().synchronize()
+            block.forward(x, None, pool.step([slot], [x.shape[0]]), y)
+            if own:
+                shape = x.shape
+                del x
+                for _ in range(4):
+                    torch.full(shape, float("nan"), dtype=BF, device=DEV)
+                    torch.full((512,), -1, dtype=torch.int32, device=DEV)
+            ys.append(y)
+        torch.cuda.synchronize()
+        outs.append(torch.cat(ys))
+    assert torch.equal(*outs)

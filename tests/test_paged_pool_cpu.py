@@ -37,7 +37,7 @@ def test_refusals_change_nothing():
     a, b = p.open(), p.open()
     p.step([a], [40])
     before = ([list(x) for x in p.owned], list(p.free), list(p.length))
-    for slots, new, kw in (([a, b], [20, 49], {}), ([a], [25], {}), ([a, a], [1, 1], {}), ([2], [1], {}), ([b], [-1], {}), ([a, b], [1], {}),
+    for slots, new, kw in (([a, b], [20, 49], {}), ([a], [25], {}), ([a, a], [1, 1], {}), ([2], [1], {}), ([-1], [1], {}), ([3], [1], {}), ([b], [-1], {}), ([a, b], [1], {}),
                            ([b], [5], dict(n_rows=4))):
         with pytest.raises(RuntimeError):
             p.step(slots, new, **kw)
@@ -46,5 +46,6 @@ def test_refusals_change_nothing():
     with pytest.raises(RuntimeError):
         p.open()
     p.close(b)
-    with pytest.raises(RuntimeError):
-        p.close(b)
+    for slot in (b, -1, 3):
+        with pytest.raises(RuntimeError):
+            p.close(slot)

@@ -470,6 +470,8 @@ typedef struct hi_paged_batch {
  *   workspace_dev: DEVICE, hi_paged_workspace_bytes bytes, filled with zeros once before its first use; a call leaves it fit
  *   for the next one.  Calls that may overlap in time need workspaces of their own, as do captured graphs that may.
  *   A row's sums may be cut differently when batch or hint change; the same call gives the same bits.
+ *   Numbers that are not finite reach only the rows that see them: an element of V that element of the output (as NaN, or as
+ *   the formula has it), a row of K, or a row's scale, all of it.
  * All buffers 16-byte aligned, the arrays of the batch 4-byte; cache and batch are HOST structs, read before the call returns;
  * n_seqs = 0 or n_rows = 0 does nothing.  Errors: HI_ERR_ARG, HI_ERR_UNSUPPORTED, HI_ERR_RANGE (a table of more
  * than 2^30 rows, more than 65535 query heads, or more work than the kernels count: 2e9 tiles of 32 keys, all sequences of the

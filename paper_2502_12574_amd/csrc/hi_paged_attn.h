@@ -22,6 +22,28 @@ constexpr int kPagedImageFloats = 66 * 256;
 // Tiles (and starts) of all blocks, in 31 bits with something to spare for the kernels' fp32 estimates of it.
 constexpr float kPagedMostTiles = 2.0e9f;
 
+// Values that are not finite.  A weight of zero takes a key out of a row only as long as its value is finite, and in a tile whose keys
+// some rows see and others don't no value can be taken out for all of them.  Where such a tile holds a value that is not finite, its
+// second product is done with zeros in their place, and a product of ones (of such values) and ones (of keys that are seen) says which
+// elements of which rows they belong to: those become NaN.
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {                 // bits 15 and 31: of the two bf16 numbers
+  return (w & 0x7F807F80u) + 0x00800080u;
+}
+__device__ __forceinline__ uint32_t spread_halves(uint32_t bits) {           // bits 15 and 31 to all of their halves
+  return ((bits >> 15) & 0x00010001u) * 0xFFFFu;
+}
+struct TwoParts { bf16x8 finite, others; };                                  // the second: ones
+__device__ __forceinline__ TwoParts two_parts(bf16x8 v) {
+  u32x4 x = __builtin_bit_cast(u32x4, v), y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t bad = spread_halves(not_finite(x[e]));
+    y[e] = bad & 0x3F803F80u;
+    x[e] &= ~bad;
+  }
+  return {__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y)};
+}
+
 struct PagedAttnArgs {
   PagedPool pool; PagedSeqs seqs;
   const uint16_t* q; uint16_t* out;

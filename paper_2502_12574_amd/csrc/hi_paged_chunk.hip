@@ -208,6 +208,7 @@ __device__ __forceinline__ void write_row(const PagedAttnArgs& a, const ChunkWor
 template <int BITS>
 __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds_raw[kLds<BITS>];
+  __shared__ int notes[2][4];
   lds_char* const lds = (lds_char*)lds_raw;
   const int lane = lane_id(), wave = wave_id(), hl = lane >> 5, col = lane & 31;
   const uint32_t size = chunk_piece(a, lane);
@@ -302,6 +303,32 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
       if (lane < 32) *(lds_float*)(lds + kScalesAt + ((stage * 2 + (lane >> 4)) * kTileRows + 16 * wave + (lane & 15)) * 4) = lane < 16 ? row_scale * a.c : row_scale;
     }
   };
+  // Values that are not finite in a tile of keys that some rows of the block see and others don't: each wavefront looks at the rows that it
+  // brought before the barrier that begins the tile, and notes it for all (of two tiles in turn, and for good: what it costs is time).
+  auto look = [&](int stage) __attribute__((always_inline)) {
+    lds_char* const at = lds + stage * kStageBytes + kTileBytes + wave * 4096 + lane * 16;
+    uint32_t bad = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x4 v = *(lds_u32x4*)(at + i * 1024);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) bad |= not_finite(v[e]);
+    }
+    bool any = (bad & 0x80008000u) != 0;
+    if (BITS == 8) any |= !(fabsf(*(lds_float*)(lds + kScalesAt + ((stage * 2 + 1) * kTileRows + 16 * wave + (lane & 15)) * 4)) < __builtin_inff());
+    if (__builtin_amdgcn_ballot_w64(any) != 0 && lane == 0) notes[stage][wave] = 1;
+  };
+  auto noted = [&](int stage) __attribute__((always_inline)) {
+    return __builtin_amdgcn_readfirstlane(notes[stage][0] | notes[stage][1] | notes[stage][2] | notes[stage][3]) != 0;
+  };
+  auto clean = [&](int stage) __attribute__((always_inline)) {          // zeros in their place, once all wavefronts know them
+    __syncthreads();
+    lds_char* const at = lds + stage * kStageBytes + kTileBytes + wave * 4096 + lane * 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *(lds_bf16x8*)(at + i * 1024) = two_parts(*(lds_bf16x8*)(at + i * 1024)).finite;
+    __syncthreads();
+  };
+  if (lane == 0) notes[0][wave] = notes[1][wave] = 0;
   fetch(0, 0);
   if (BITS == 8 && threadIdx.x < kTileRows) *(lds_float*)(lds + kOnesAt + threadIdx.x * 4) = 1.f;
   const float unit = BITS == 8 ? 1.f : a.c;      // what scores and maxima are multiplied by before the power of two
@@ -341,11 +368,14 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
   for (int j = 0; j < n; ++j) {
     const int stage = j & 1, key0 = (w.t0 + j) * kTileRows;
     if constexpr (BITS == 16) wait_vmcnt<0>();
+    const bool hides = key0 + kTileRows - 1 > w.sees;
+    if (hides) look(stage);
     __syncthreads();
     if (j + 1 < n) fetch(j + 1, 1 - stage);
     lds_char* const kt = lds + stage * kStageBytes;
     lds_char* const vt = kt + kTileBytes;
     if (!works) {                                // (no row of the wavefront's is a row of the block)
+      if (hides && noted(stage)) clean(stage);
       if (j + 1 < n) settle(1 - stage);
       continue;
     }
@@ -356,11 +386,12 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
     bf16x8 op[A + 1];
     f32x16 s[2];
     auto read_k = [&](int i) __attribute__((always_inline)) { op[i % (A + 1)] = *(lds_bf16x8*)(kt + lc.koff[i >> 1] + (i & 1) * 8192); };
-    auto read_v = [&](int i) __attribute__((always_inline)) {
+    auto v_operand = [&](int i) __attribute__((always_inline)) {
       lds_char* const p = vt + lc.voff[i & 3] + (i >> 2) * 4096;
       const bf16x4 v0 = lds_read_tr8(p), v1 = lds_read_tr8(p + 2048);
-      op[i % (A + 1)] = (bf16x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+      return (bf16x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
     };
+    auto read_v = [&](int i) __attribute__((always_inline)) { op[i % (A + 1)] = v_operand(i); };
 #pragma unroll
     for (int r = 0; r < 16; ++r) { s[0][r] = 0.f; s[1][r] = 0.f; }
 #pragma unroll
@@ -373,7 +404,6 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
       __builtin_amdgcn_sched_barrier(0);
     }
     lds_char* const sc = lds + kScalesAt + stage * 2 * kTileRows * 4 + 16 * hl;
-    const bool hides = key0 + kTileRows - 1 > w.sees;
     lds_char* by_key = sc;                       // what the scores are still to be multiplied by
     if (hides || holes) {
       if constexpr (BITS == 8) {
@@ -469,6 +499,39 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
     }
     st.l += sum;
     __builtin_amdgcn_sched_barrier(0);
+    uint32_t marks[2] = {0, 0};                  // bit 16 (db % 2) + r of db / 2: NaN belongs there
+    if (hides && noted(stage)) {
+      const uint64_t shown = (lim - key0 >= 63 ? ~0ull : lim < key0 ? 0ull : (2ull << (lim - key0)) - 1) >> (4 * hl);
+      const uint32_t upto[2] = {(uint32_t)shown, (uint32_t)(shown >> 32)};
+      auto mask_of = [&](int i, int e) __attribute__((always_inline)) {      // of the two keys of a word of the weights
+        const uint32_t two = upto[i >> 1] >> (16 * (i & 1) + 8 * (e >> 1) + 2 * (e & 1));
+        return (two & 1) * 0xFFFFu | (two & 2) * 0x7FFF8000u;
+      };
+#pragma unroll
+      for (int db = 0; db < 4; ++db) {
+        f32x16 hit;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) hit[r] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          u32x4 seen;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            seen[e] = 0x3F803F80u & mask_of(i, e);
+            if (BITS == 8 && db == 0) pw[i >> 1][i & 1][e] &= mask_of(i, e);       // (a scale that is not finite)
+          }
+          hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(two_parts(v_operand(4 * i + db)).others, __builtin_bit_cast(bf16x8, seen), hit, 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) marks[db >> 1] |= (hit[r] > 0.f ? 1u : 0u) << (16 * (db & 1) + r);
+      }
+      clean(stage);
+      if (BITS == 16) {
+#pragma unroll
+        for (int i = 0; i < A; ++i) read_v(i);
+      }
+    }
     if constexpr (BITS == 8) {
 #pragma unroll
       for (int i = 0; i < A; ++i) read_v(i);
@@ -478,6 +541,12 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
       if (i + A < 16) read_v(i + A);
       st.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i % (A + 1)], __builtin_bit_cast(bf16x8, pw[i >> 3][(i >> 2) & 1]), st.o[i & 3], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
+    }
+    if (__builtin_amdgcn_ballot_w64((marks[0] | marks[1]) != 0) != 0) {
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st.o[db][r] = marks[db >> 1] >> (16 * (db & 1) + r) & 1 ? __builtin_nanf("") : st.o[db][r];
     }
     if (j + 1 < n) settle(1 - stage);
   }

@@ -127,9 +127,10 @@ __device__ __forceinline__ bf16x8 two_words(uint32_t w0, uint32_t w1) {       //
 }
 
 // One tile, its halves at at[0] and at[1].  Register r of half h of the lane (column lane % 16, g4 = lane / 16) is key 16 h + 4 g4 + r, and
-// the contraction of the second product takes them in that order, h, then r.  hides: only the keys up to lim[h] of a half count.
+// the contraction of the second product takes them in that order, h, then r.  hides: only the keys up to lim[h] of a half count; differ: and
+// they are not the same ones for all columns.
 template <int BITS>
-__device__ __forceinline__ void attend_tile(lds_char* const (&at)[2], int lane, const bf16x8 (&qf)[4], RowState& st, float c, bool hides, const int (&lim)[2]) {
+__device__ __forceinline__ void attend_tile(lds_char* const (&at)[2], int lane, const bf16x8 (&qf)[4], RowState& st, float c, bool hides, bool differ, const int (&lim)[2]) {
   typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
   typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
   typedef __attribute__((address_space(3))) uint64_t lds_u64;
@@ -223,7 +224,35 @@ __device__ __forceinline__ void attend_tile(lds_char* const (&at)[2], int lane, 
       for (int r = 0; r < 4; ++r) p[h][r] *= vs[h][r];
   }
   // the weights are rounded to bf16 for the matrix pipe (2^-9 of each at most); their sum is that of the fp32 values
-  const u32x4 pw = {pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]), pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])};
+  u32x4 pw = {pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]), pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])};
+  if (hides && differ) {
+    uint32_t bad = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (BITS == 8) bad |= not_finite(pw[e]);                   // (a scale that is not)
+#pragma unroll
+      for (int db = 0; db < 8; ++db) bad |= not_finite(__builtin_bit_cast(u32x4, vop[db])[e]);
+    }
+    if (__builtin_amdgcn_ballot_w64((bad & 0x80008000u) != 0) != 0) {
+      u32x4 seen;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int h = e >> 1, r = 4 * g4 + 2 * (e & 1);
+        const uint32_t shown = (r <= lim[h] ? 0xFFFFu : 0u) | (r + 1 <= lim[h] ? 0xFFFF0000u : 0u);
+        pw[e] &= shown;
+        seen[e] = 0x3F803F80u & shown;
+      }
+#pragma unroll
+      for (int db = 0; db < 8; ++db) {
+        const TwoParts v = two_parts(vop[db]);
+        const f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.others, __builtin_bit_cast(bf16x8, seen), (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+        st.o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.finite, __builtin_bit_cast(bf16x8, pw), st.o[db], 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) st.o[db][r] = hit[r] > 0.f ? __builtin_nanf("") : st.o[db][r];
+      }
+      return;
+    }
+  }
 #pragma unroll
   for (int db = 0; db < 8; ++db) st.o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop[db], __builtin_bit_cast(bf16x8, pw), st.o[db], 0, 0, 0);
 }
@@ -486,7 +515,7 @@ __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
       if (ok0 || ok1) {
         lds_char* const halves[2] = {(lds_char*)(uintptr_t)(ring + slot * R::kSlot), (lds_char*)(uintptr_t)(ring + (slot + 1) * R::kSlot)};
         const int lims[2] = {ok0 ? lim - row : -1, ok1 ? lim - row - 16 : -1};
-        attend_tile<BITS>(halves, lane, qf, st, a.c, row + kTile - 1 > all_see || !ok0 || !ok1, lims);
+        attend_tile<BITS>(halves, lane, qf, st, a.c, row + kTile - 1 > all_see || !ok0 || !ok1, rows > 1, lims);
       }
       asm volatile("" ::: "memory");
       slot = slot + 2 < R::kSlots ? slot + 2 : 0;

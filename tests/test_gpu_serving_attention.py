@@ -122,6 +122,50 @@ def test_infinite_and_nan_values_reach_only_rows_that_see_them(hint):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("past,new,kw", [
+    ([100, 0], [4, 2], dict(group=4)), ([30], [90], dict(group=1, kv_heads=1, page=32)), ([5, 64, 200], [200, 33, 1], dict(group=4)),
+    ([3000], [70], dict(group=8, kv_heads=1, page=64)), ([17], [150], dict(group=3, page=128))])
+def test_infinite_and_nan_rows_of_a_step_reach_only_later_rows(past, new, kw, bits):
+    """Rows at the end of a sequence's new ones: an element of V, a row's scale, a row of K that is not finite."""
+    b = Batch(past, new, bits=bits, seed=10, **kw)
+    q = b.rows(b.H * b.G)
+    values = b.values()
+    clean = {hint: attend(b, q, max_rows=hint) for hint in (1, 1 << 20)}
+    bad = torch.zeros(q.shape, dtype=torch.bool)
+
+    def poison(s, back, head, which, channel=None, x=float("nan")):
+        """the row `back` from the sequence's last one, seen by the last back + 1 query rows"""
+        pos = past[s] + new[s] - 1 - back
+        page, r = b.table[s][pos // b.page], pos % b.page
+        if channel is not None and bits == 16:
+            b.pages[page, head, which, r, channel] = x
+        elif channel is not None:
+            b.pages.view(torch.uint8)[page, head, which, r, channel] = 0xFF
+        elif bits == 8:
+            b.scales[page, head, which, r] = x
+        else:
+            b.pages[page, head, which, r] = x
+        every = channel is None or which == 0
+        at = slice(b.starts[s + 1] - 1 - back, b.starts[s + 1])
+        bad[head * b.G:(head + 1) * b.G, at, slice(None) if every else channel] = True
+
+    last = b.H - 1
+    poison(0, 0, 0, 1, 7, float("inf"))
+    poison(0, 1, 0, 1, 100, float("-inf"))
+    poison(0, 2, 0, 1, 33)
+    if new[0] > 40:
+        poison(0, 25, 0, 1, 64, float("inf"))
+    if len(new) > 1:
+        poison(1, 0, last, 1, None, float("inf"))
+        poison(1, 1, 0, 0, 5)
+    bad = bad.to(DEV)
+    for hint, want in clean.items():
+        got = attend(b, q, max_rows=hint)
+        assert not torch.isfinite(got[bad]).any(), hint
+        attention_close(torch.where(bad, want, got), q, values, b, what=hint)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("past,new,hint", [([20000, 100, 3000], [1, 1, 1], 1), ([9000, 50], [3, 90], 1 << 20)])
 def test_attention_gives_the_same_bits_again(bits, past, new, hint):
     b = Batch(past, new, bits=bits, seed=12, page=64)

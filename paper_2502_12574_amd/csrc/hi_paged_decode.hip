@@ -23,6 +23,7 @@ namespace hi {
 namespace {
 
 constexpr int kTile = 32;
+constexpr int kShortTable = 1024;               // entries of a page table that are brought to LDS at once
 constexpr int kCols = 16;
 
 // A slot of a ring holds half a tile, 16 rows.
@@ -344,11 +345,18 @@ __device__ __forceinline__ void gather_pieces(int n, At piece_at, int cols, floa
   }
 }
 
+// n / d for quotients of a few hundred at most (by_d: 1 / d, nearly)
+__device__ __forceinline__ uint32_t small_quotient(uint32_t n, uint32_t d, float by_d) {
+  const uint32_t q = (uint32_t)((float)n * by_d);
+  const int rest = (int)(n - q * d);
+  return rest < 0 ? q - 1 : rest >= (int)d ? q + 1 : q;
+}
+
 template <int BITS>
 __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
   using R = Ring<BITS>;
   extern __shared__ __attribute__((aligned(1024))) char lds_raw[];
-  __shared__ int arrived;
+  __shared__ int arrived, short_table[kShortTable];
   const int lane = lane_id(), wave = wave_id(), g4 = lane >> 4, col = lane & 15;
   const int S = a.seqs.n_seqs, shift = a.pool.shift, page_rows = 1 << shift;
   const uint32_t ring = (uint32_t)(uintptr_t)(lds_char*)lds_raw + wave * kWaveLds<BITS>;
@@ -361,35 +369,45 @@ __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
     mine = s0 + lane < S ? paged_seq_of(a.seqs, s0 + lane) : PagedSeq{0, 0, 0};
     mw = seq_work(a, mine);
   };
+  // A short table is brought along with the lengths: the pages of a tile are known one latency earlier.
+  const int64_t all_entries = (int64_t)S * a.seqs.table_pages;
+  const int entries = all_entries <= kShortTable ? (int)all_entries : 0;
+  if (S <= 64) look(0);
+  int brought[kShortTable / 256];
+#pragma unroll
+  for (int i = 0; i < kShortTable / 256; ++i) brought[i] = (int)threadIdx.x + 256 * i < entries ? a.seqs.table[threadIdx.x + 256 * i] : 0;
   constexpr int kStart = kPagedStart<BITS>;
   int tiles_of_all = 0, items_of_all = 0;
   float about = 0.f;                                               // (a batch whose sequences overlap could overflow the count)
   for (int s0 = 0; s0 < S; s0 += 64) {
-    look(s0);
+    if (S > 64) look(s0);
     tiles_of_all += __builtin_amdgcn_readlane(sum_wave(mw.tiles * mw.items), 63);
     items_of_all += __builtin_amdgcn_readlane(sum_wave(mw.items), 63);
     about += over_wave((float)(mw.tiles + kStart) * (float)mw.items, op_add);
   }
   if (about > 1.01f * kPagedMostTiles) return;
-  const uint32_t wgs = gridDim.x;
+  constexpr uint32_t wgs = kPagedRuns;
   // equal pieces: as small as a workgroup each allows, or a quarter larger
   uint32_t piece_tiles = ((uint32_t)tiles_of_all + wgs - 1) / wgs;
   piece_tiles = piece_tiles < kPagedLeastRun ? kPagedLeastRun : piece_tiles;
   int pieces = 0;
   bool by_piece = false;
+  float by_tiles = 0.f;
+  auto pieces_of = [&](int tiles) __attribute__((always_inline)) { return (int)small_quotient(tiles + piece_tiles - 1, piece_tiles, by_tiles); };
 #pragma unroll
   for (int attempt = 0; attempt < 2 && !by_piece; ++attempt) {
     if (attempt == 1) piece_tiles += piece_tiles / 4 + 1;
-    pieces = 0;                                                    // (at most as many as tiles)
+    pieces = 0;                                                    // (at most as many as tiles; of a block, twice wgs at most)
+    by_tiles = __builtin_amdgcn_rcpf((float)piece_tiles);
     for (int s0 = 0; s0 < S; s0 += 64) {
       if (S > 64) look(s0);
-      pieces += __builtin_amdgcn_readlane(sum_wave((int)((mw.tiles + piece_tiles - 1) / piece_tiles) * mw.items), 63);
+      pieces += __builtin_amdgcn_readlane(sum_wave(pieces_of(mw.tiles) * mw.items), 63);
     }
     by_piece = pieces <= (int)wgs;
   }
   const int total = tiles_of_all + kStart * items_of_all, run = (int)(((uint32_t)total + wgs - 1) / wgs);
   // From here on a block has units: its start and its tiles, or its equal pieces if a workgroup takes one of them.
-  auto units_of = [&](int tiles) __attribute__((always_inline)) { return by_piece ? (int)((tiles + piece_tiles - 1) / piece_tiles) : tiles + kStart; };
+  auto units_of = [&](int tiles) __attribute__((always_inline)) { return by_piece ? pieces_of(tiles) : tiles + kStart; };
   const int step = by_piece ? 1 : run, all = by_piece ? pieces : total, start = by_piece ? 0 : kStart;
   int at = blockIdx.x * step;
   if (at >= all) return;
@@ -406,6 +424,11 @@ __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
     }
     before += __builtin_amdgcn_readlane(upto, 63);
     seq = s0 + 64;
+  }
+  if (entries != 0) {
+#pragma unroll
+    for (int i = 0; i < kShortTable / 256; ++i) short_table[threadIdx.x + 256 * i] = brought[i];
+    __syncthreads();
   }
   const int looked = S > 64 ? seq & ~63 : 0;                       // the lanes hold the 64 sequences from here on
 
@@ -433,8 +456,12 @@ __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
     const int b = (int)((uint32_t)item / (uint32_t)a.pool.heads), kv = item - b * a.pool.heads;
     const int u0 = at - begin, u1 = (end < done ? end : done) - begin;
     if (u1 <= start) return;                                       // (a run that ends in a block's start: the next one begins it)
-    const int t0 = by_piece ? (int)((uint64_t)w.tiles * (uint32_t)u0 / (uint32_t)units) : u0 > start ? u0 - start : 0;
-    const int t1 = by_piece ? (int)((uint64_t)w.tiles * (uint32_t)u1 / (uint32_t)units) : u1 - start;
+    int t0 = u0 > start ? u0 - start : 0, t1 = u1 - start;
+    if (by_piece) {                                                // (one piece: u1 = u0 + 1)
+      const int each = (int)((uint32_t)w.tiles / (uint32_t)units), longer = w.tiles - each * units;
+      t0 = each * u0 + (u0 < longer ? u0 : longer);
+      t1 = t0 + each + (u0 < longer ? 1 : 0);
+    }
 
     const int row0 = sq.first + b * a.positions;
     const int rows = sq.rows - b * a.positions < a.positions ? sq.rows - b * a.positions : a.positions;
@@ -457,7 +484,8 @@ __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
     auto half_row = [&](int h) __attribute__((always_inline)) { return (t0 + wave + 4 * (h >> 1)) * kTile + 16 * (h & 1); };
     auto pages_from = [&](int h) __attribute__((always_inline)) {
       const int row = half_row(h + lane);
-      return h + lane < 2 * n && row < len ? table[row >> shift] : -1;
+      if (h + lane >= 2 * n || row >= len) return -1;
+      return entries != 0 ? short_table[seq * a.seqs.table_pages + (row >> shift)] : table[row >> shift];
     };
     int pages = pages_from(0), pages_next = 0, base = 0;
 

@@ -279,20 +279,27 @@ __global__ __launch_bounds__(64 * W, (Few<RX, NT, U, W, S>::kPerSimd)) void line
   }
 }
 
-// ---- more rows: the matrix rate is the bound.  A workgroup takes 128 rows and 128 outputs, a group of 128 channels at a time; a
-// wavefront takes all rows and 32 of the outputs, so that no code is expanded twice in a workgroup.  x goes to LDS by direct loads, a
-// step ahead, the codes into registers.  Operands are read four ahead of the products that take them (left to itself the compiler reads
+// ---- more rows: the matrix rate is the bound.  A workgroup takes 32 RT rows (128; 96 where that fills the chip better) and 128 outputs, a
+// group of 128 channels at a time; a wavefront takes all rows and 32 of the outputs, so that no code is expanded twice in a workgroup.  x goes to LDS by direct loads, a
+// step ahead, the codes into registers.  Operands are read RT ahead of the products that take them (left to itself the compiler reads
 // each where it is needed, and the products wait for LDS: 4096 x 4096 and 1500 rows 101 us).
 // The sums' part of an output, (z - 16 s) sum x, is a 32x32x16 product of its own for each group: a row's sum as three bf16 numbers
 // (24 bits of it), and 16 times them, against z and -s.  Each wavefront forms the sums of 32 rows, from the operands that it reads
-// anyway, for all four; they are used a step later.
-constexpr int kQTile = 128;
-constexpr int kQStage = kQTile * 256;                    // x of a group
-constexpr int kQSums = 2 * kQStage;                      // [stage][row] 8 numbers of a row's sum, then 16 bytes of zeros
-constexpr int kQZeros = kQSums + 2 * kQTile * 16;
-constexpr int kQLds = kQZeros + 16;
+// anyway, for all; they are used a step later.
+constexpr int kQTile = 128;                              // outputs
+template <int RT>
+struct Tile {
+  static constexpr int kRows = 32 * RT;
+  static constexpr int kStage = kRows * 256;             // x of a group
+  static constexpr int kSums = 2 * kStage;               // [stage][row] 8 numbers of a row's sum, then 16 bytes of zeros
+  static constexpr int kZeros = kSums + 2 * kRows * 16;
+  static constexpr int kLds = kZeros + 16;
+};
 
+template <int RT>
 __global__ __launch_bounds__(256, 2) void linear_tile_kernel(LinearArgs a, int row_tiles) {
+  using T = Tile<RT>;
+  constexpr int kQStage = T::kStage, kQSums = T::kSums, kQZeros = T::kZeros, kQLds = T::kLds, kRows = T::kRows;
   typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
   typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
   __shared__ __attribute__((aligned(1024))) char lds_raw[kQLds];
@@ -302,28 +309,28 @@ __global__ __launch_bounds__(256, 2) void linear_tile_kernel(LinearArgs a, int r
   const int per = (gridDim.x + 7) / 8, at = (blockIdx.x & 7) * per + (blockIdx.x >> 3), n_tiles = (a.n_out + kQTile - 1) / kQTile;
   const int band = at / (8 * n_tiles), in = at - band * 8 * n_tiles, high = row_tiles - 8 * band < 8 ? row_tiles - 8 * band : 8;
   if (high <= 0) return;
-  const int row0 = (8 * band + in % high) * kQTile, n0 = in / high * kQTile;
+  const int row0 = (8 * band + in % high) * kRows, n0 = in / high * kQTile;
   if (n0 >= a.n_out) return;
   const int n = n0 + 32 * wave + col, nc = n < a.n_out ? n : a.n_out - 1;
   const char* const codes = a.codes + (int64_t)nc * (a.n_in / 2) + 32 * hl;
   const uint16_t* const sp = a.scales + (int64_t)nc * groups;
   const uint16_t* const zp = a.zeros + (int64_t)nc * groups;
 
-  // x: the wavefront brings rows 32 wave .. of a tile, 4 to a load (chunk p of row r is chunk p ^ (r % 16) of its 256 bytes)
+  // x: the wavefront brings rows 8 RT wave .. of a tile, 4 to a load (chunk p of row r is chunk p ^ (r % 16) of its 256 bytes)
   const uint32_t pitch = a.x_heads ? 2 * kQGroup : 2u * a.n_in;
   const char* x_now = (const char*)a.x + (int64_t)row0 * pitch;
   const int64_t x_step = a.x_heads ? (int64_t)a.rows * (2 * kQGroup) : 2 * kQGroup;
-  const uint32_t lds_wave = (uint32_t)(uintptr_t)lds + wave * 8192;
-  uint32_t x_off[8];
+  const uint32_t lds_wave = (uint32_t)(uintptr_t)lds + wave * (RT * 2048);
+  uint32_t x_off[2 * RT];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int r = 32 * wave + 4 * i + (lane >> 4);
+  for (int i = 0; i < 2 * RT; ++i) {
+    const int r = 8 * RT * wave + 4 * i + (lane >> 4);
     x_off[i] = (uint32_t)(row0 + r < a.rows ? r : a.rows - 1 - row0) * pitch + (((lane & 15) ^ (r & 15)) << 4);
   }
   struct Codes { u32x4 w[2]; uint32_t s, z; };
   auto fetch = [&](Codes& b, int g, int stage) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) g2lds16_s<0>(x_now, x_off[i], lds_wave + stage * kQStage + i * 1024);
+    for (int i = 0; i < 2 * RT; ++i) g2lds16_s<0>(x_now, x_off[i], lds_wave + stage * kQStage + i * 1024);
     x_now += x_step;
     b.w[0] = *(const u32x4*)(codes + (int64_t)g * 64);
     b.w[1] = *(const u32x4*)(codes + (int64_t)g * 64 + 16);
@@ -331,45 +338,46 @@ __global__ __launch_bounds__(256, 2) void linear_tile_kernel(LinearArgs a, int r
     b.z = zp[g];
   };
   if (threadIdx.x == 0) *(lds_u32x4*)(lds + kQZeros) = (u32x4){0, 0, 0, 0};
-  // x operand j of channels 64 hl + 8 k ..: row tile j ^ wave, the wavefront's own first; bits 4 .. 6 change with k
-  uint32_t x_at[4], sum_at[4];
+  // x operand j of channels 64 hl + 8 k ..: the row tiles from the wavefront's own on; bits 4 .. 6 change with k
+  auto row_tile = [&](int j) __attribute__((always_inline)) { return wave + j < RT ? wave + j : (wave + j) % RT; };
+  uint32_t x_at[RT], sum_at[RT];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    x_at[j] = (uint32_t)(((j ^ wave) * 32 + col) * 256 + (((8 * hl) ^ (col & 15)) << 4));
-    sum_at[j] = hl ? kQZeros : kQSums + ((j ^ wave) * 32 + col) * 16;
+  for (int j = 0; j < RT; ++j) {
+    x_at[j] = (uint32_t)((row_tile(j) * 32 + col) * 256 + (((8 * hl) ^ (col & 15)) << 4));
+    sum_at[j] = hl ? kQZeros : kQSums + (row_tile(j) * 32 + col) * 16;
   }
-  const uint32_t my_sum = kQSums + (wave * 32 + col) * 16;
-  f32x16 y[4];
+  const uint32_t my_sum = kQSums + (row_tile(0) * 32 + col) * 16;      // (two wavefronts write the same sums where RT is 3)
+  f32x16 y[RT];
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
+  for (int t = 0; t < RT; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) y[t][r] = 0.f;
   const CodeBits bits;
   u32x4 zs = {0, 0, 0, 0};                       // the last step's z and -s
   auto add_sums = [&](int stage) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read16(lds + sum_at[j] + (hl ? 0 : stage * (kQTile * 16))), __builtin_bit_cast(bf16x8, zs), y[j], 0, 0, 0);
+    for (int j = 0; j < RT; ++j)
+      y[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lds_read16(lds + sum_at[j] + (hl ? 0 : stage * (kRows * 16))), __builtin_bit_cast(bf16x8, zs), y[j], 0, 0, 0);
   };
   auto step = [&](int g, auto parity, Codes& now, Codes& next) __attribute__((always_inline)) {
-    constexpr int stage = decltype(parity)::value, A = 4;
+    constexpr int stage = decltype(parity)::value, A = RT;
     wait_vmcnt<0>();
     asm volatile("" : "+v"(now.w[0]), "+v"(now.w[1]), "+v"(now.s), "+v"(now.z));      // (they were asked for a step ago)
     __syncthreads();
     if (g + 1 < groups) fetch(next, g + 1, 1 - stage);
     lds_char* const xt = lds + stage * kQStage;
-    f32x16 acc[4];
+    f32x16 acc[RT];
     bf16x8 op[A + 1], b[2];
     float sum = 0.f;
-    auto read = [&](int i) __attribute__((always_inline)) { op[i % (A + 1)] = lds_read16(xt + (x_at[i & 3] ^ ((i >> 2) << 4))); };
+    auto read = [&](int i) __attribute__((always_inline)) { op[i % (A + 1)] = lds_read16(xt + (x_at[i % RT] ^ ((i / RT) << 4))); };
 #pragma unroll
     for (int i = 0; i < A; ++i) read(i);
     b[0] = codes_to_bf16(now.w[0][0], bits);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const int k = i >> 2, j = i & 3;
-      if (i + A < 32) read(i + A);
+    for (int i = 0; i < 8 * RT; ++i) {
+      const int k = i / RT, j = i % RT;
+      if (i + A < 8 * RT) read(i + A);
       f32x16 z;
 #pragma unroll
       for (int r = 0; r < 16; ++r) z[r] = 0.f;
@@ -392,10 +400,10 @@ __global__ __launch_bounds__(256, 2) void linear_tile_kernel(LinearArgs a, int r
     const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
     sum = __uint_as_float(halves[0]) + __uint_as_float(halves[1]);
     const float h = bf16_bits_to_float((uint16_t)pack_bf16(sum, 0.f)), m = bf16_bits_to_float((uint16_t)pack_bf16(sum - h, 0.f)), l = sum - h - m;
-    *(lds_u32x4*)(lds + my_sum + stage * (kQTile * 16)) = (u32x4){pack_bf16(h, m), pack_bf16(l, 16.f * h), pack_bf16(16.f * m, 16.f * l), 0u};
+    *(lds_u32x4*)(lds + my_sum + stage * (kRows * 16)) = (u32x4){pack_bf16(h, m), pack_bf16(l, 16.f * h), pack_bf16(16.f * m, 16.f * l), 0u};
     const float s = __uint_as_float(now.s << 16);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < RT; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) y[j][r] = __builtin_fmaf(s, acc[j][r], y[j][r]);
   };
@@ -411,10 +419,10 @@ __global__ __launch_bounds__(256, 2) void linear_tile_kernel(LinearArgs a, int r
   add_sums((groups - 1) & 1);
   if (n >= a.n_out) return;
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
+  for (int t = 0; t < RT; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int row = row0 + 32 * (t ^ wave) + 8 * (r >> 2) + 4 * hl + (r & 3);
+      const int row = row0 + 32 * row_tile(t) + 8 * (r >> 2) + 4 * hl + (r & 3);
       if (row < a.rows) *y_at(a, row, n) = (uint16_t)pack_bf16(y[t][r], 0.f);
     }
 }
@@ -430,6 +438,13 @@ hipError_t few_go(hipStream_t s, const LinearArgs& a) {
                      F::kLds, s, a);
   return hipSuccess;
 }
+template <int RT>
+hi_status tile_go(hipStream_t s, const LinearArgs& a) {
+  const int64_t row_tiles = ceil_div(a.rows, 32 * RT), tiles = row_tiles * ceil_div(a.n_out, kQTile);
+  if (tiles > (1 << 24) - 8) { set_last_error("quantised linear: too many rows"); return HI_ERR_RANGE; }
+  hipLaunchKernelGGL(linear_tile_kernel<RT>, dim3((unsigned)(8 * ceil_div(tiles, 8))), dim3(256), 0, s, a, (int)row_tiles);
+  return launched("quantised linear");
+}
 // turns of 4 groups, as long as each wavefront has one
 template <int RX, int NT, int W, int S>
 hipError_t few_turns(hipStream_t s, const LinearArgs& a) {
@@ -437,21 +452,28 @@ hipError_t few_turns(hipStream_t s, const LinearArgs& a) {
   return groups >= 4 * W ? few_go<RX, NT, 4, W, S>(s, a) : groups >= 2 * W ? few_go<RX, NT, 2, W, S>(s, a) : few_go<RX, NT, 1, W, S>(s, a);
 }
 
-// Rows of a workgroup: 16, 32 or 64 in the kernel for few rows, 128 in the other.  Microseconds of each, from the rounds that its
-// workgroups take (g: groups of channels; two workgroups of the first and the last fit a compute unit, one of the others), fitted to
-// hidden sizes of 1024 to 8192 and 1 to 4096 rows.  Measured there, at 4096 x 4096: 64 rows 12.1 with 64 a workgroup, 256 rows 25 and,
-// with 128, 45, 512 rows 48 and 46, 1024 rows 94 and 47; at 8192 x 8192: 256 rows 88 and 85.
+// Rows of a workgroup: 16, 32 or 64 in the kernel for few rows, 96 or 128 in the other.  Microseconds of each, from the rounds that its
+// workgroups take (g: groups of channels; two workgroups of the first and of the last two fit a compute unit, one of the others), fitted
+// to hidden sizes of 1024 to 8192 and 1 to 4096 rows.  Measured there, at 4096 x 4096: 64 rows 12.1 with 64 a workgroup; 256 rows 27, with
+// 96 and 128 38 and 45; 512 rows 48, 40 and 47; 1024 rows 94, 56 and 50; 1500 rows, 96 and 128: 67 and 72, 2048 rows 97 and 86; at
+// 8192 x 8192: 256 rows 88, 72 and 85.
 int linear_form(int64_t rows, int64_t n_out, int g) {
   auto few = [&](int64_t r, int64_t outs) { return ceil_div(rows, r) * ceil_div(n_out, outs); };
-  const int64_t w16 = few(16, 16), w32 = few(32, 32), w64 = few(64, 32), t = few(kQTile, kQTile), rest = t % 512;
-  const double us[4] = {1.3 + (w16 <= 256 ? 0.11 * g : (double)ceil_div(w16, 512) * 0.18 * g),
+  auto tiles = [&](int64_t t, double full, double half) {
+    const int64_t rest = t % 512;
+    const double last = rest == 0 ? 0 : rest <= 256 ? half : half + (full - half) * (0.35 + 0.65 / 256 * (double)(rest - 256));
+    return 3 + ((double)(t / 512) * full + last) * g;
+  };
+  const int64_t w16 = few(16, 16), w32 = few(32, 32), w64 = few(64, 32);
+  const int forms[5] = {16, 32, 64, 96, 128};
+  const double us[5] = {1.3 + (w16 <= 256 ? 0.11 * g : (double)ceil_div(w16, 512) * 0.18 * g),
                         1.3 + (double)ceil_div(w32, 256) * (0.5 + 0.18 * g),
                         1.5 + (double)ceil_div(w64, 256) * (1.5 + 0.30 * g),
-                        (double)(t / 512) * (3 + 2.5 * g) + (rest == 0 ? 0 : rest <= 256 ? 3 + 1.33 * g : 3 + 2.4 * g)};
-  int best = 3;
-  for (int i = 0; i < 3; ++i)
-    if (us[i] < us[best] && ceil_div(rows, 16 << i) <= 65535) best = i;       // (the second dimension of a grid ends there)
-  return 16 << best;
+                        tiles(few(96, kQTile), 1.97, 1.12), tiles(few(128, kQTile), 2.48, 1.33)};
+  int best = 4;
+  for (int i = 3; i >= 0; --i)
+    if (us[i] < us[best] && (i == 3 || ceil_div(rows, forms[i]) <= 65535)) best = i;       // (the second dimension of a grid ends there)
+  return forms[best];
 }
 
 }  // namespace
@@ -510,11 +532,8 @@ extern "C" hi_status hi_linear_quantized(void* stream, const void* x_dev, const 
     case 16: e = few_turns<4, 1, 8, 2>(st, a); break;
     case 32: e = few_turns<8, 2, 8, 2>(st, a); break;
     case 64: e = few_turns<16, 2, 4, 2>(st, a); break;
-    default: {
-      const int64_t row_tiles = ceil_div(n_rows, kQTile), tiles = row_tiles * ceil_div(n_out, kQTile);
-      if (tiles > (1 << 24) - 8) { set_last_error("quantised linear: too many rows"); return HI_ERR_RANGE; }
-      hipLaunchKernelGGL(linear_tile_kernel, dim3((unsigned)(8 * ceil_div(tiles, 8))), dim3(256), 0, st, a, (int)row_tiles);
-    }
+    case 96: return tile_go<3>(st, a);
+    default: return tile_go<4>(st, a);
   }
   if (e != hipSuccess) { set_last_error("quantised linear: %s", hipGetErrorString(e)); return HI_ERR_HIP; }
   return launched("quantised linear");

@@ -53,7 +53,8 @@ def test_linear(rows, n_in, n_out):
             check(got, x, codes, scale, zero, (rows, n_in, n_out, xh, yh))
 
 
-@pytest.mark.parametrize("rows,n_in,n_out", [(1, 4096, 6144), (5, 8192, 1024), (40, 4096, 4096), (300, 4096, 2048), (1100, 1024, 1168)])
+@pytest.mark.parametrize("rows,n_in,n_out", [(1, 4096, 6144), (5, 8192, 1024), (40, 4096, 4096), (300, 4096, 2048), (1100, 1024, 1168),
+                                             (700, 4096, 4096), (1490, 2048, 1936)])
 def test_linear_at_model_sizes(rows, n_in, n_out):
     codes, scale, zero = weights(n_out, n_in, 7)
     x = torch.randn(rows, n_in, generator=torch.Generator().manual_seed(rows)).to(BF).to(DEV)

@@ -18,9 +18,21 @@ constexpr int kPagedPieceFloats = 16 * kPartialFloats;
 constexpr int kPagedSlots = 512;
 constexpr int kPagedMostImages = 4 * kPagedSlots + 16;
 constexpr int kPagedImageFloats = 66 * 256;
+constexpr int kPagedFan = 3, kPagedLevels = 4;   // log2 of the images of a merge; their levels
+static_assert(1 << (kPagedFan * kPagedLevels) >= kPagedMostImages, "a block's images");
+constexpr int kPagedCounts = kPagedLevels * kPagedMostImages;
 
 // Tiles (and starts) of all blocks, in 31 bits with something to spare for the kernels' fp32 estimates of it.
 constexpr float kPagedMostTiles = 2.0e9f;
+
+// Numbers that another workgroup reads: two at a time, by accesses that no L2 keeps a copy of.
+__device__ __forceinline__ void store_shared2(float* p, float x, float y) {
+  __hip_atomic_store((uint64_t*)p, (uint64_t)__float_as_uint(x) | ((uint64_t)__float_as_uint(y) << 32), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_shared2(const float* p) {
+  const uint64_t v = __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
 
 // Values that are not finite.  A weight of zero takes a key out of a row only as long as its value is finite, and in a tile whose keys
 // some rows see and others don't no value can be taken out for all of them.  Where such a tile holds a value that is not finite, its
@@ -50,7 +62,7 @@ struct PagedAttnArgs {
   int group;
   int positions, by_group;       // positions of a block; 65536 / group, rounded up
   float c;                       // what a score is multiplied by before the power of two
-  int* arrivals; int* plan; float* pieces; float* images;   // in the workspace
+  int* arrivals; int* counts; float* pieces; float* images;   // in the workspace
 };
 
 hi_status launch_paged_decode(void* stream, const PagedAttnArgs& a);

@@ -5,8 +5,9 @@ namespace hi {
 
 namespace {
 
-// The workspace: arrival counts, the length of a piece, then either the pieces of the one kernel or the images of the other.
-constexpr int kArrivalBytes = kPagedArrivals * 4 + 256;
+// The workspace: the arrival counts of both kernels, then either the pieces of the one or the images of the other.
+constexpr int kArrivalBytes = (kPagedArrivals + kPagedCounts) * 4;
+static_assert(kArrivalBytes % 256 == 0, "aligned images");
 
 }  // namespace
 
@@ -43,7 +44,7 @@ extern "C" hi_status hi_paged_attn(void* stream, const hi_paged_cache* cache, co
   a.group = group;
   a.c = softmax_scale_log2(q_prescaled != 0);
   a.arrivals = (int*)workspace_dev;
-  a.plan = a.arrivals + kPagedArrivals;
+  a.counts = a.arrivals + kPagedArrivals;
   a.pieces = a.images = (float*)((char*)workspace_dev + kArrivalBytes);
   a.by_group = (65536 + group - 1) / group;
   const bool few = (int64_t)batch->max_rows * group <= 16;

@@ -2,15 +2,16 @@
 //
 // Work.  A block is 128 rows of one sequence and one KV head: 128 / group consecutive positions with the query heads of that KV head,
 // so that its rows share the keys.  It sweeps its sequence's keys in tiles of 64; a workgroup takes a block, or, where long blocks alone
-// would not fill the chip, one of the equal pieces into which all blocks of the sequence are cut (merged by paged_merge_kernel).  Every
-// workgroup works the cut out from the lengths themselves, so a captured launch follows them.  KV heads change fastest in the
-// numbering, then blocks, deep ones first: with 8 heads each XCD sweeps one of them, and the workgroups that sweep the same tiles at
+// would not fill the chip, one of the equal pieces into which all blocks of the sequence are cut.  Pieces are merged by the workgroups that
+// finish last (a launch of its own for that was 3 us dearer where nothing is cut, and nearly as much where few are).  Every workgroup
+// works the cut out from the lengths themselves, so a captured launch follows them.  KV heads change fastest in the numbering, then blocks, deep ones first: with 8 heads each XCD sweeps one of them, and the workgroups that sweep the same tiles at
 // the same time find them in its L2.  (Runs of equal numbers of tiles, as for few rows, would lose that.)
 //
 // A wavefront holds 32 rows.  S^T = K Q^T (32x32x16 tiles) leaves a row in one lane column: its running maximum and sum are per lane,
 // and the weights, rounded to bf16, are the B operand of O^T += V^T P^T as they lie.  bf16 tiles go to LDS by direct loads; rows of
 // 8 bits pass through registers, where they become bf16 (exactly) once for the whole workgroup, and their scales multiply scores
-// and weights in fp32 (that of a K row in the operation that takes the reference off its scores: it is brought along times c).  Two workgroups a compute unit hide each other's softmax.
+// and weights in fp32 (that of a K row in the operation that takes the reference off its scores: it is brought along times c).  Two
+// workgroups a compute unit hide each other's softmax.
 #include "hi_paged_attn.h"
 
 namespace hi {
@@ -84,12 +85,13 @@ __device__ __forceinline__ SeqBlocks seq_blocks(const PagedAttnArgs& a, const Pa
 __device__ __forceinline__ int pieces_of(int tiles, uint32_t piece) { return (int)((tiles + piece - 1) / piece); }
 
 // What a workgroup does: its block, and the tiles [t0, t1) of it; pieces of the block, the block's first image and the distance of the
-// next piece's (number: the workgroup's, or with MERGE the block's).
+// next piece's (number: the workgroup's).
 struct ChunkWork { int seq, kv, row0, rows, tiles, t0, t1, sees, len, pieces, piece, image, next_image; bool any; };
 // The tiles of a piece: whole blocks, or pieces of an even share of the tiles of all blocks over one round of workgroups, an eighth or a
 // quarter more of it (an even share often leaves a few pieces for a round of their own), or over two rounds.  A workgroup costs 6 tiles
-// to begin and to end, a merge 3 and one for every 70 images, and a round ends with its longest piece unless the short ones that
+// to begin and to end, merges 3 and one for every 70 pieces, and a round ends with its longest piece unless the short ones that
 // follow fill its gaps.  0: there is nothing to do.
+// (Merges at 6 whatever the pieces: 8 x 512 rows behind 2000 97 us instead of 84.6.)
 // 384 rows behind 8000, 96 blocks of 131 tiles: 89 us with even shares (576 pieces), 79 with an eighth more (480).
 __device__ __forceinline__ uint32_t chunk_piece(const PagedAttnArgs& a, int lane) {
   const int S = a.seqs.n_seqs;
@@ -125,10 +127,16 @@ __device__ __forceinline__ uint32_t chunk_piece(const PagedAttnArgs& a, int lane
       best = size;
     }
   }
-  return __builtin_amdgcn_readfirstlane((uint32_t)best);
+  const uint32_t piece = __builtin_amdgcn_readfirstlane((uint32_t)best);
+  // (sequences that overlap could have more pieces than there are workgroups: a merge would wait for the next call)
+  uint32_t pieces = 0;
+  for (int s0 = 0; s0 < S; s0 += 64) {
+    if (S > 64) look(s0);
+    pieces += __builtin_amdgcn_readlane(sum_wave((int)blocks * pieces_of((int)tiles, piece)), 63);
+  }
+  return pieces <= gridDim.x ? piece : 0;
 }
 
-template <bool MERGE>
 __device__ __forceinline__ ChunkWork chunk_work(const PagedAttnArgs& a, uint32_t piece, int number, int lane) {
   ChunkWork w;
   w.any = false;
@@ -144,7 +152,7 @@ __device__ __forceinline__ ChunkWork chunk_work(const PagedAttnArgs& a, uint32_t
   int before = 0, images = 0, seq = 0, n_blocks = 0, k = 1;
   for (int s0 = 0; s0 < S; s0 += 64) {
     look(s0);
-    const int cut = pieces_of(sb.tiles, piece), here = sb.blocks * H * (MERGE ? 1 : cut), kept = cut > 1 ? sb.blocks * H * cut : 0;
+    const int cut = pieces_of(sb.tiles, piece), here = sb.blocks * H * cut, kept = cut > 1 ? sb.blocks * H * cut : 0;
     const int upto = sum_wave(here), images_upto = sum_wave(kept);
     const int n = __popcll(__builtin_amdgcn_ballot_w64(before + upto <= number));
     if (n < 64) {
@@ -172,7 +180,6 @@ __device__ __forceinline__ ChunkWork chunk_work(const PagedAttnArgs& a, uint32_t
   w.kv = (int)(in - of_all * H);
   w.piece = (int)(of_all / (uint32_t)n_blocks);
   const int nth = (int)of_all - w.piece * n_blocks, b = n_blocks - 1 - nth;      // the deepest first
-  w.pieces = k;
   w.next_image = n_blocks * H;
   w.image = images + nth * H + w.kv;
   w.row0 = first + b * a.positions;
@@ -182,9 +189,13 @@ __device__ __forceinline__ ChunkWork chunk_work(const PagedAttnArgs& a, uint32_t
   const int64_t sees = (int64_t)past + b * a.positions, deepest = sees + w.rows;
   w.sees = (int)(sees < w.len ? sees : w.len - 1);                               // the last key of the block's first position
   w.tiles = (int)(((deepest < w.len ? deepest : w.len) + kTileRows - 1) / kTileRows);
-  w.t0 = (int)((uint64_t)w.tiles * (uint32_t)w.piece / (uint32_t)k);
-  w.t1 = (int)((uint64_t)w.tiles * (uint32_t)(w.piece + 1) / (uint32_t)k);
-  w.any = true;
+  // the pieces are equal; a block of fewer tiles than pieces has that many
+  k = k < w.tiles ? k : w.tiles;
+  const int each = (int)((uint32_t)w.tiles / (uint32_t)k), longer = w.tiles - each * k;
+  w.pieces = k;
+  w.t0 = each * w.piece + (w.piece < longer ? w.piece : longer);
+  w.t1 = w.t0 + each + (w.piece < longer ? 1 : 0);
+  w.any = w.piece < k;
   return w;
 }
 
@@ -208,13 +219,11 @@ __device__ __forceinline__ void write_row(const PagedAttnArgs& a, const ChunkWor
 template <int BITS>
 __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds_raw[kLds<BITS>];
-  __shared__ int notes[2][4];
+  __shared__ int notes[2][4], arrived;
   lds_char* const lds = (lds_char*)lds_raw;
   const int lane = lane_id(), wave = wave_id(), hl = lane >> 5, col = lane & 31;
-  const uint32_t size = chunk_piece(a, lane);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.plan = (int)size;        // for the merge
-  const ChunkWork w = chunk_work<false>(a, size, blockIdx.x, lane);
-  if (!w.any || w.t0 >= w.t1) return;
+  const ChunkWork w = chunk_work(a, chunk_piece(a, lane), blockIdx.x, lane);
+  if (!w.any) return;
   const int n = w.t1 - w.t0;
   const int* const table = a.seqs.table + (int64_t)w.seq * a.seqs.table_pages;
   const int in_page = (1 << a.pool.shift) - 1;
@@ -551,87 +560,90 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
     if (j + 1 < n) settle(1 - stage);
   }
 
-  if (!works) return;
-  const float l = both_halves(st.l, false);
-  if (w.pieces == 1) {
-    const float inv = l > 0.f ? 1.0f / l : 0.f;
-    if (mine.live) {
+  float m = st.m, l = both_halves(st.l, false);
+  if (w.pieces > 1) {
+    // The block's pieces are merged eight at a time, by the workgroup that finishes last of the eight, then eight of those; in the pieces'
+    // order, whoever it is.  An image's numbers are written and read by accesses that no L2 keeps a copy of (the wait for the stores, the
+    // barrier and the count order them).
+    float* const images = a.images + (int64_t)w.image * kPagedImageFloats + 2 * threadIdx.x;
+    const int64_t next = (int64_t)w.next_image * kPagedImageFloats;
+    auto keep = [&](int p) __attribute__((always_inline)) {
+      float* const to = images + p * next;
 #pragma unroll
-      for (int db = 0; db < 4; ++db) write_row(a, w, mine, db, hl, st.o[db], inv);
-    }
-    return;
-  }
-  float* const image = a.images + (int64_t)(w.image + w.piece * w.next_image) * kPagedImageFloats + threadIdx.x;
+      for (int i = 0; i < 32; ++i) store_shared2(to + i * 512, st.o[i >> 3][2 * (i & 7)], st.o[i >> 3][2 * (i & 7) + 1]);
+      store_shared2(to + 32 * 512, m, l);
+    };
+    if (works) keep(w.piece);
+    for (int level = 0, lead = w.piece;; ++level) {
+      const int shift = kPagedFan * level, first = lead >> (shift + kPagedFan) << (shift + kPagedFan);
+      const int there = ((w.pieces - first - 1) >> shift) + 1, of = there < (1 << kPagedFan) ? there : 1 << kPagedFan;
+      const bool all = w.pieces <= 1 << (shift + kPagedFan);
+      lead = first;
+      if (of > 1) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0) {
+          int* const count = a.counts + level * kPagedMostImages + w.image + first * w.next_image;
+          arrived = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
+          if (arrived == of) __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (arrived != of) return;
+        if (works) {
+          const float* const from = images + first * next;
+          const int64_t step = next << shift;
+          float2 ml[1 << kPagedFan];
+          m = kNegBig;
 #pragma unroll
-  for (int db = 0; db < 4; ++db)
+          for (int i = 0; i < 1 << kPagedFan; ++i) ml[i] = i < of ? load_shared2(from + i * step + 32 * 512) : make_float2(kNegBig, 0.f);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) image[(db * 16 + r) * 256] = st.o[db][r];
-  image[64 * 256] = st.m;
-  image[65 * 256] = l;
-}
-
-// Joins the pieces of a block: a workgroup for each 32 dims of it, in the lanes of the kernel above.
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
-  const int lane = lane_id(), wave = wave_id(), db = blockIdx.y;
-  const ChunkWork w = chunk_work<true>(a, (uint32_t)*a.plan, blockIdx.x, lane);
-  if (!w.any || w.pieces == 1 || 32 * wave >= w.rows * a.group) return;
-  const LaneRow mine = lane_row(a, w, 32 * wave + (lane & 31));
-  const float* const images = a.images + (int64_t)w.image * kPagedImageFloats + threadIdx.x;
-  const int64_t next = (int64_t)w.next_image * kPagedImageFloats;
-  // (a block with fewer tiles than pieces has left no image for some of them)
-  auto left = [&](int p) __attribute__((always_inline)) {
-    return (uint64_t)w.tiles * (uint32_t)p / (uint32_t)w.pieces < (uint64_t)w.tiles * (uint32_t)(p + 1) / (uint32_t)w.pieces;
-  };
-  const float unit = a.pool.bits == 8 ? 1.f : a.c;
-  float m = kNegBig, l = 0.f;
-  f32x16 o;
+          for (int i = 0; i < 1 << kPagedFan; ++i) m = fmaxf(m, ml[i].x);
+          l = 0.f;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) o[r] = 0.f;
-  constexpr int N = 4;                           // pieces whose loads are under way together
-  for (int p0 = 0; p0 < w.pieces; p0 += N) {
-    float pm[N], pl[N];
-    f32x16 po[N];
+          for (int db = 0; db < 4; ++db)
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      pm[i] = kNegBig;
-      pl[i] = 0.f;
+            for (int r = 0; r < 16; ++r) st.o[db][r] = 0.f;
+          float2 x[2][32];                       // an image, and the next one under way
+          auto bring = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) po[i][r] = 0.f;
-      if (p0 + i < w.pieces && left(p0 + i)) {
-        const float* const x = images + (p0 + i) * next;
-        pm[i] = x[64 * 256];
-        pl[i] = x[65 * 256];
+            for (int e = 0; e < 32; ++e) x[i & 1][e] = load_shared2(from + i * step + e * 512);
+            __builtin_amdgcn_sched_barrier(0);
+          };
+          bring(0);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) po[i][r] = x[(db * 16 + r) * 256];
+          for (int i = 0; i < 1 << kPagedFan; ++i) {
+            if (i >= of) break;
+            if (i + 1 < of) bring(i + 1);
+            const float f = fast_exp2((ml[i].x - m) * unit);
+            l += f * ml[i].y;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              st.o[e >> 3][2 * (e & 7)] += f * x[i & 1][e].x;
+              st.o[e >> 3][2 * (e & 7) + 1] += f * x[i & 1][e].y;
+            }
+          }
+        }
       }
-    }
-    const float mn = fmaxf(fmaxf(fmaxf(pm[0], pm[1]), fmaxf(pm[2], pm[3])), m), f = fast_exp2((m - mn) * unit);
-    m = mn;
-    l *= f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[r] *= f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float e = fast_exp2((pm[i] - m) * unit);
-      l += e * pl[i];
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[r] += e * po[i][r];
+      if (all) break;
+      if (works && of > 1) keep(lead);
     }
   }
-  if (mine.live) write_row(a, w, mine, db, lane >> 5, o, l > 0.f ? 1.0f / l : 0.f);
+  const float inv = l > 0.f ? 1.0f / l : 0.f;
+  if (works && mine.live) {
+#pragma unroll
+    for (int db = 0; db < 4; ++db) write_row(a, w, mine, db, hl, st.o[db], inv);
+  }
 }
 
 }  // namespace
 
-// units: at least as many as there are blocks; their pieces are at most 2 x 512 more
+// units: at least as many as there are blocks; a block that is cut has at most a piece more than its share of the 2 x 512, and the whole
+// pieces of all are no more than those
 hi_status launch_paged_chunk(void* stream, const PagedAttnArgs& a, int64_t units) {
   const dim3 grid((unsigned)(units + 2 * kPagedSlots));
   if (a.pool.bits == 16) hipLaunchKernelGGL(paged_chunk_kernel<16>, grid, dim3(256), 0, (hipStream_t)stream, a);
   else hipLaunchKernelGGL(paged_chunk_kernel<8>, grid, dim3(256), 0, (hipStream_t)stream, a);
-  const hi_status st = launched("paged attention");
-  if (st != HI_OK) return st;
-  hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned)units, 4), dim3(256), 0, (hipStream_t)stream, a);
-  return launched("paged attention merge");
+  return launched("paged attention");
 }
 
 }  // namespace hi

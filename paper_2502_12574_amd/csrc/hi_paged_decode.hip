@@ -52,14 +52,6 @@ __device__ __forceinline__ void wait_halves(int newer) {
   else wait_halves<LOADS, MOST - 2>(newer);
 }
 
-__device__ __forceinline__ void store_shared2(float* p, float x, float y) {
-  __hip_atomic_store((uint64_t*)p, (uint64_t)__float_as_uint(x) | ((uint64_t)__float_as_uint(y) << 32), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 load_shared2(const float* p) {
-  const uint64_t v = __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
-}
-
 struct RowState {
   float m, l;
   f32x4 o[8];

@@ -165,6 +165,20 @@ def test_infinite_and_nan_rows_of_a_step_reach_only_later_rows(past, new, kw, bi
         attention_close(torch.where(bad, want, got), q, values, b, what=hint)
 
 
+@pytest.mark.parametrize("hint", [1, 64])
+def test_overlapping_sequences_leave_the_workspace_fit(hint):
+    """Row starts that go back give rows to several sequences (their outputs are anyone's); the call after it is as ever."""
+    b = Batch([300] * 299, [1] * 299, page=64, seed=14, kv_heads=1)
+    q, ws = b.rows(4), b.workspace()
+    cache, batch = b.structs(hint)
+    starts = batch._keepalive[2]
+    starts.copy_(torch.tensor([0, 299] * 150))
+    hb.hi_paged_attn(torch.cuda.current_stream(), cache, batch, q, 4, 0, torch.empty_like(q), ws)
+    first = attend(b, q, 0, hint, ws)
+    attention_close(first, q, b.values(), b)
+    assert torch.equal(attend(b, q, 0, hint), first)
+
+
 @pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("past,new,hint", [([20000, 100, 3000], [1, 1, 1], 1), ([9000, 50], [3, 90], 1 << 20)])
 def test_attention_gives_the_same_bits_again(bits, past, new, hint):

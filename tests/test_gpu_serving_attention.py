@@ -180,7 +180,7 @@ def test_overlapping_sequences_leave_the_workspace_fit(hint):
 
 
 @pytest.mark.parametrize("bits", [16, 8])
-@pytest.mark.parametrize("past,new,hint", [([20000, 100, 3000], [1, 1, 1], 1), ([9000, 50], [3, 90], 1 << 20)])
+@pytest.mark.parametrize("past,new,hint", [([20000, 100, 3000], [1, 1, 1], 1), ([9000, 50], [3, 90], 1 << 20), ([40000], [5], 1 << 20)])
 def test_attention_gives_the_same_bits_again(bits, past, new, hint):
     b = Batch(past, new, bits=bits, seed=12, page=64)
     q, ws = b.rows(8), b.workspace()

@@ -1,11 +1,14 @@
 // Attention of a chunk of new rows of each of many sequences over a pool of cache pages: the matrix rate is the bound.
+// 4001 rows of 32 + 8 heads behind 28639: 1850 to 1950 us from box to box, 1.03 to 1.08 PFLOP/s at the clock that the power limit leaves
+// (about 1.96 GHz; the matrix pipe is busy 52 % of the time and the vector pipe as long); 8-bit pages 2130 to 2270.
 //
 // Work.  A block is 128 rows of one sequence and one KV head: 128 / group consecutive positions with the query heads of that KV head,
 // so that its rows share the keys.  It sweeps its sequence's keys in tiles of 64; a workgroup takes a block, or, where long blocks alone
 // would not fill the chip, one of the equal pieces into which all blocks of the sequence are cut.  Pieces are merged by the workgroups that
 // finish last (a launch of its own for that was 3 us dearer where nothing is cut, and nearly as much where few are).  Every workgroup
-// works the cut out from the lengths themselves, so a captured launch follows them.  KV heads change fastest in the numbering, then blocks, deep ones first: with 8 heads each XCD sweeps one of them, and the workgroups that sweep the same tiles at
-// the same time find them in its L2.  (Runs of equal numbers of tiles, as for few rows, would lose that.)
+// works the cut out from the lengths themselves, so a captured launch follows them.  KV heads change fastest in the numbering, then
+// blocks, deep ones first: with 8 heads each XCD sweeps one of them, and the workgroups that sweep the same tiles at the same time find
+// them in its L2.  (Runs of equal numbers of tiles, as for few rows, would lose that.)
 //
 // A wavefront holds 32 rows.  S^T = K Q^T (32x32x16 tiles) leaves a row in one lane column: its running maximum and sum are per lane,
 // and the weights, rounded to bf16, are the B operand of O^T += V^T P^T as they lie.  bf16 tiles go to LDS by direct loads; rows of

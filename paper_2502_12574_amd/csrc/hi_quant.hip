@@ -13,7 +13,7 @@ constexpr int kQMostIn = 1 << 20;               // 64 rows of x, or 16 of codes,
 constexpr int kQMostOut = 1 << 24;              // (a launch has at most 2^32 lanes)
 
 // ---- bf16 weights to codes: a wavefront takes 16 groups at a time, 4 lanes a group with 32 channels each.  The weights are read
-// once and a quarter of them written; run once per matrix.
+// once and a quarter of them written; run once per matrix (8192 x 8192: 30 us, 5.7 TB/s).
 __global__ __launch_bounds__(256) void weight_quant_kernel(const uint16_t* __restrict__ w, int64_t groups, char* __restrict__ codes,
                                                            uint16_t* __restrict__ scales, uint16_t* __restrict__ zeros) {
   const int64_t at = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 2);
@@ -111,7 +111,8 @@ __device__ __forceinline__ uint16_t* y_at(const LinearArgs& a, int row, int n) {
 // ---- up to 64 rows: the read of the weights is the bound.  A workgroup takes 16 NT outputs and all rows (4 RX of them); its W
 // wavefronts take turns of U consecutive groups each and add their sums through LDS.  Codes and x come through a private LDS ring of S
 // groups a wavefront, by direct loads: as the matrix tiles want them, 16 neighbouring lanes would touch 16 rows, and the look-up of
-// their lines, not the bytes, would be the bound (16 rows of 4096 x 6144: 13.0 us with loads into registers).  Sums of x come
+// their lines, not the bytes, would be the bound (16 rows of 4096 x 6144: 13.0 us with loads into registers).  One row 5.6 us (2.4 TB/s:
+// a chain of launch, ring and join), 29 rows of 8192 x 8192 13.5 us (2.7 TB/s: the feed of the rings).  Sums of x come
 // out of the matrix pipe too, against ones.
 // A workgroup begins its turns where its number says: the rows of codes lie a power of two apart, and workgroups that all began at
 // the first channel would keep to a few memory channels.
@@ -280,9 +281,11 @@ __global__ __launch_bounds__(64 * W, (Few<RX, NT, U, W, S>::kPerSimd)) void line
 }
 
 // ---- more rows: the matrix rate is the bound.  A workgroup takes 32 RT rows (128; 96 where that fills the chip better) and 128 outputs, a
-// group of 128 channels at a time; a wavefront takes all rows and 32 of the outputs, so that no code is expanded twice in a workgroup.  x goes to LDS by direct loads, a
-// step ahead, the codes into registers.  Operands are read RT ahead of the products that take them (left to itself the compiler reads
-// each where it is needed, and the products wait for LDS: 4096 x 4096 and 1500 rows 101 us).
+// group of 128 channels at a time; a wavefront takes all rows and 32 of the outputs, so that no code is expanded twice in a workgroup.
+// x goes to LDS by direct loads, a step ahead, the codes into registers.  Operands are read RT ahead of the products that take them (left
+// to itself the compiler reads each where it is needed, and the products wait for LDS: 4096 x 4096 and 1500 rows 101 us, with the reads
+// ahead 72, in tiles of 96 rows 65).  8192 x 8192 and 4096 rows: 623 us, 880 TFLOP/s; the products and the operations that make and feed
+// their operands take turns.
 // The sums' part of an output, (z - 16 s) sum x, is a 32x32x16 product of its own for each group: a row's sum as three bf16 numbers
 // (24 bits of it), and 16 times them, against z and -s.  Each wavefront forms the sums of 32 rows, from the operands that it reads
 // anyway, for all; they are used a step later.

@@ -121,10 +121,10 @@ __device__ __forceinline__ bf16x8 two_words(uint32_t w0, uint32_t w1) {       //
 }
 
 // One tile, its halves at at[0] and at[1].  Register r of half h of the lane (column lane % 16, g4 = lane / 16) is key 16 h + 4 g4 + r, and
-// the contraction of the second product takes them in that order, h, then r.  hides: only the keys up to lim[h] of a half count; differ: and
-// they are not the same ones for all columns.
+// the contraction of the second product takes them in that order, h, then r.  hides: only the keys up to lim[h] of a half count; later: and
+// others may be rows (behind the last row lie only copies of it).
 template <int BITS>
-__device__ __forceinline__ void attend_tile(lds_char* const (&at)[2], int lane, const bf16x8 (&qf)[4], RowState& st, float c, bool hides, bool differ, const int (&lim)[2]) {
+__device__ __forceinline__ void attend_tile(lds_char* const (&at)[2], int lane, const bf16x8 (&qf)[4], RowState& st, float c, bool hides, bool later, const int (&lim)[2]) {
   typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
   typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
   typedef __attribute__((address_space(3))) uint64_t lds_u64;
@@ -219,7 +219,7 @@ __device__ __forceinline__ void attend_tile(lds_char* const (&at)[2], int lane, 
   }
   // the weights are rounded to bf16 for the matrix pipe (2^-9 of each at most); their sum is that of the fp32 values
   u32x4 pw = {pack_bf16(p[0][0], p[0][1]), pack_bf16(p[0][2], p[0][3]), pack_bf16(p[1][0], p[1][1]), pack_bf16(p[1][2], p[1][3])};
-  if (hides && differ) {
+  if (hides && later) {
     uint32_t bad = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -468,6 +468,7 @@ __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
       return (int)(key < len ? key : len - 1);
     };
     const int lim = sees(pos), all_see = sees(0);
+    const bool later = all_see < len - 1;                          // rows that some column does not see
     const int* const table = a.seqs.table + (int64_t)seq * a.seqs.table_pages;
     const char* const of_head = a.pool.pages + (uint64_t)head_bytes * (uint32_t)kv;
     const char* const scales_of_head = (const char*)a.pool.scales + ((uint64_t)(uint32_t)kv << (shift + 3));
@@ -536,7 +537,7 @@ __global__ __launch_bounds__(256, 2) void paged_decode_kernel(PagedAttnArgs a) {
       if (ok0 || ok1) {
         lds_char* const halves[2] = {(lds_char*)(uintptr_t)(ring + slot * R::kSlot), (lds_char*)(uintptr_t)(ring + (slot + 1) * R::kSlot)};
         const int lims[2] = {ok0 ? lim - row : -1, ok1 ? lim - row - 16 : -1};
-        attend_tile<BITS>(halves, lane, qf, st, a.c, row + kTile - 1 > all_see || !ok0 || !ok1, rows > 1, lims);
+        attend_tile<BITS>(halves, lane, qf, st, a.c, row + kTile - 1 > all_see || !ok0 || !ok1, later, lims);
       }
       asm volatile("" ::: "memory");
       slot = slot + 2 < R::kSlots ? slot + 2 : 0;

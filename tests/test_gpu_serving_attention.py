@@ -124,7 +124,8 @@ def test_infinite_and_nan_values_reach_only_rows_that_see_them(hint):
 @pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("past,new,kw", [
     ([100, 0], [4, 2], dict(group=4)), ([30], [90], dict(group=1, kv_heads=1, page=32)), ([5, 64, 200], [200, 33, 1], dict(group=4)),
-    ([3000], [70], dict(group=8, kv_heads=1, page=64)), ([17], [150], dict(group=3, page=128))])
+    ([3000], [70], dict(group=8, kv_heads=1, page=64)), ([17], [150], dict(group=3, page=128)), ([40], [5], dict(group=16, kv_heads=1)),
+    ([8, 90], [60, 3], dict(group=11))])
 def test_infinite_and_nan_rows_of_a_step_reach_only_later_rows(past, new, kw, bits):
     """Rows at the end of a sequence's new ones: an element of V, a row's scale, a row of K that is not finite."""
     b = Batch(past, new, bits=bits, seed=10, **kw)

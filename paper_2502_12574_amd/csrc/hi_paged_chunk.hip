@@ -238,7 +238,21 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
     const int row = group_row(j + lane);
     return j + lane < n && row < w.len ? table[row >> a.pool.shift] : -1;
   };
+  // what the piece begins with is asked for at once: the pages of its first tiles, of the search for holes, queries (then the first tile)
   int pages = pages_from(0);
+  const int first_page = w.t0 * kTileRows >> a.pool.shift, last_page = ((w.t1 * kTileRows < w.len ? w.t1 * kTileRows : w.len) - 1) >> a.pool.shift;
+  const int first_pages = table[first_page + lane < last_page ? first_page + lane : last_page];
+  const LaneRow mine = lane_row(a, w, 32 * wave + col);
+  bf16x8 qf[8];
+  {
+    const uint16_t* const q = a.q + ((int64_t)(w.kv * a.group + mine.g) * a.seqs.n_rows + w.row0 + mine.pos) * kHeadDim + 8 * hl;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      uint4 raw = make_uint4(0, 0, 0, 0);
+      if (mine.live) raw = *(const uint4*)(q + 16 * kk);
+      qf[kk] = __builtin_bit_cast(bf16x8, raw);
+    }
+  }
   auto page_of = [&](int j) __attribute__((always_inline)) {
     if (j > 0 && (j & 63) == 0) pages = pages_from(j);
     return __builtin_amdgcn_readlane(pages, j & 63);
@@ -346,23 +360,9 @@ __global__ __launch_bounds__(256, 2) void paged_chunk_kernel(PagedAttnArgs a) {
   const float unit = BITS == 8 ? 1.f : a.c;      // what scores and maxima are multiplied by before the power of two
 
   // rows that a piece's tiles lack because their page is not there: looked for once
-  bool holes = false;
-  for (int p = w.t0 * kTileRows >> a.pool.shift; p <= ((w.t1 * kTileRows < w.len ? w.t1 * kTileRows : w.len) - 1) >> a.pool.shift; p += 64) {
-    const int i = p + lane, end = ((w.t1 * kTileRows < w.len ? w.t1 * kTileRows : w.len) - 1) >> a.pool.shift;
-    holes |= __builtin_amdgcn_ballot_w64(i <= end && !there(table[i <= end ? i : end])) != 0;
-  }
+  bool holes = __builtin_amdgcn_ballot_w64(!there(first_pages)) != 0;
+  for (int p = first_page + 64; p <= last_page; p += 64) holes |= __builtin_amdgcn_ballot_w64(!there(table[p + lane < last_page ? p + lane : last_page])) != 0;
 
-  const LaneRow mine = lane_row(a, w, 32 * wave + col);
-  bf16x8 qf[8];
-  {
-    const uint16_t* const q = a.q + ((int64_t)(w.kv * a.group + mine.g) * a.seqs.n_rows + w.row0 + mine.pos) * kHeadDim + 8 * hl;
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) {
-      uint4 raw = make_uint4(0, 0, 0, 0);
-      if (mine.live) raw = *(const uint4*)(q + 16 * kk);
-      qf[kk] = __builtin_bit_cast(bf16x8, raw);
-    }
-  }
   const int lim = w.sees + mine.pos < w.len ? w.sees + mine.pos : w.len - 1;     // the last key the lane's row sees
   const bool works = 32 * wave < w.rows * a.group;
   const Lane lc = lane_offsets(lane);

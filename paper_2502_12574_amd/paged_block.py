@@ -89,17 +89,19 @@ class PagePool:
             raise RuntimeError("a sequence would outgrow max_context")
         if sum(need) > len(self.free):                       # before anything changes hands
             raise RuntimeError(f"{sum(need)} pages wanted, {len(self.free)} free")
-        past, starts, table = [], [0], []
+        fresh = iter(reversed(self.free))
+        past, starts, table = [self.length[s] for s in slots], [0], []
         for s, n, m in zip(slots, new_rows, need):
-            self.owned[s] += [self.free.pop() for _ in range(m)]
-            past.append(self.length[s])
             starts.append(starts[-1] + n)
-            self.length[s] += n
-            table.append(self.owned[s])
+            table.append(self.owned[s] + [next(fresh) for _ in range(m)])
         width = max([len(t) for t in table] + [1])
         rows = [t + [-1] * (width - len(t)) for t in table]
         flat = torch.tensor(past + starts + [p for row in rows for p in row], dtype=torch.int32).to(self.device)     # (one copy)
         k = len(slots)
+        del self.free[len(self.free) - sum(need):]
+        for s, n, t in zip(slots, new_rows, table):
+            self.owned[s] = t
+            self.length[s] += n
         return hb.make_paged_batch(flat[2 * k + 1:], flat[:k], flat[k:2 * k + 1], k, width, total if n_rows is None else n_rows,
                                    max(new_rows + [1]))
 

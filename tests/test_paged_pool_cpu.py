@@ -49,3 +49,19 @@ def test_refusals_change_nothing():
     for slot in (b, -1, 3):
         with pytest.raises(RuntimeError):
             p.close(slot)
+
+
+def test_a_step_that_cannot_be_copied_to_the_device_changes_nothing(monkeypatch):
+    p = pool()
+    a = p.open()
+    p.step([a], [20])
+    before = ([list(x) for x in p.owned], list(p.free), list(p.length))
+
+    def fails(*args, **kw):
+        raise MemoryError
+    with monkeypatch.context() as m:
+        m.setattr("paper_2502_12574_amd.paged_block.torch.tensor", fails)
+        with pytest.raises(MemoryError):
+            p.step([a], [20])
+    assert before == ([list(x) for x in p.owned], list(p.free), list(p.length))
+    assert rows(p.step([a], [20]))[1] == [20]
